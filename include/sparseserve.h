@@ -359,6 +359,143 @@ ss_status ss_append_kv(const void *new_kv, int32_t *len_dev, int32_t *nblk_dev, 
                        int nblk_max, void *open_blocks, void *meta, int meta_kind, int32_t *overflow,
                        void *stream);
 
+/* ------------------------------------------------- shared pool of pages
+ * Block tables and slot maps built on the GPU from the requests' lengths
+ * (Section 3.1's fixed-size blocks, for requests that join, grow and finish
+ * between steps), so that no length, table or page count visits the host.
+ * A pool of n_pages pages of blk tokens is shared by the rows of a batch.
+ * Row b's block j lies in page tables[b][j], the same for every KV head
+ * (page p of head g is a record at region_off + p * record_bytes with
+ * region_off[b*Hkv+g] = g * n_pages * record_bytes; see ss_write_kv8).  The
+ * free list is a stack: pages free_pages[0 .. n_free).
+ *   len: device int32 [B] tokens of each row; n_free: device int32 [1]
+ *   tables: device int32 [B][max_blocks], rows filled to ceil(len/blk)
+ * ss_block_tables gives the step's new tokens, n_new (device int32 [B], 0 for
+ * an idle row), their places:
+ *   tok_begin: device int32 [B+1], row b's tokens are rows tok_begin[b] ..
+ *       tok_begin[b+1]-1 of the step's token tensors (prefix sums, cut at
+ *       token_cap)
+ *   slots: device int32 [token_cap], page * blk + place of each token;
+ *   positions: the same shape, its place in the sequence (or NULL).  Both
+ *       are -1 behind the last token (a padded batch) and for tokens that
+ *       are not served
+ *   tables: an entry for every page taken.  Pages are taken from the top of
+ *       the stack, in row order; taken: device int32 [B+1], the pages taken
+ *       before each row, then all
+ *   len_out, nblk_out (or NULL): device int32 [B], tokens and full blocks
+ *       afterwards; n_free_out: device int32 [1].  len_out may be len and
+ *       n_free_out n_free
+ *   status: device int32 [B]: 0 served (also rows without new tokens); 1 the
+ *       pool has too few pages: the first row whose pages, with all before,
+ *       pass the pool and every later row that needs any; 2 the row would
+ *       pass max_blocks; 3 a negative length, or token rows past token_cap.
+ *       A row that is not served takes nothing and keeps its length.
+ * A page number outside the pool (in tables or free_pages) gives slots of -1.
+ * B up to 65536; n_pages * blk below 2^31.  One launch up to 4096 token rows,
+ * else two.
+ * ss_block_release returns the pages of finished rows (done: device int32
+ * [B], non-zero) to the stack, row after row in block order, and sets their
+ * length to 0; other rows keep theirs.  tables is not written.  len_out may
+ * be len, n_free_out n_free; nblk_out may be NULL. */
+ss_status ss_block_tables(const int32_t *len, const int32_t *n_new, const int32_t *n_free, int B, int blk,
+                          int max_blocks, int n_pages, const int32_t *free_pages, int32_t *tables, int32_t *len_out,
+                          int32_t *nblk_out, int32_t *n_free_out, int32_t *tok_begin, int32_t *slots,
+                          int32_t *positions, int token_cap, int32_t *taken, int32_t *status, void *stream);
+ss_status ss_block_release(const int32_t *len, const int32_t *done, const int32_t *n_free, int B, int blk,
+                           int max_blocks, int n_pages, const int32_t *tables, int32_t *free_pages, int32_t *len_out,
+                           int32_t *nblk_out, int32_t *n_free_out, void *stream);
+
+/* ------------------------------------------------- KV cache in 8 bits
+ * Block records with K and V codes of 8 bits and a scale for each block, head
+ * and tensor: about half the bytes of a bf16 record in HBM.  Record of one
+ * block (ss_kv8_record_bytes: 2*blk*d + 128), 16-byte aligned:
+ *     K codes, blk*d bytes; V codes, blk*d bytes;
+ *     fp32 K scale, fp32 V scale, zeros to 128 bytes
+ * Codes stand in subtiles s of T = min(blk, 16) tokens; token t of a subtile,
+ * channel c:
+ *     K: s*T*d + (c/16)*T*16 + t*16 + c%16
+ *     V: s*T*d + (c%8/4)*T*64 + (t/4)*256 + (c/8)*16 + (c%4)*4 + t%4
+ * Formats: SS_KV8_E4M3 (OCP e4m3, largest value Q = 448), SS_KV8_INT8 (two's
+ * complement, Q = 127).  With m the tile's largest magnitude, at least 2^-100:
+ * scale = m/Q, code = x * (Q/m) rounded to nearest even, each operation
+ * rounded to fp32; a value is code * scale.  A tile that holds an infinity or
+ * a NaN gets the scale NaN and codes 0.
+ * Units, region_off and slot_limit as for ss_sparse_attention: page p of unit
+ * u is the record at kv_base + region_off[u] + p * record_bytes (offsets are
+ * 64 bits), p below slot_limit. */
+#define SS_KV8_E4M3 0
+#define SS_KV8_INT8 1
+/* Bytes of a record; 0 for an unsupported blk or d.  Host-only. */
+size_t ss_kv8_record_bytes(int blk, int d);
+
+/* Writes a step's new K and V, any number of tokens per sequence.  Every
+ * block that fills is quantised once, from bf16, into the record of its
+ * page; the tokens of a block that does not fill are kept in bf16 in the
+ * sequence's open record (row / column p = position % blk, the layout of
+ * ss_append_kv), from which a later call completes the block.
+ *   k, v: device bf16; token i of head g is d values at + i*tok_stride +
+ *       g*head_stride (bytes, multiples of 16; a fused [tokens][Hkv][2][d]
+ *       tensor is v = k + d values, tok_stride Hkv*4*d, head_stride 4*d)
+ *   tok_begin: device int32 [B+1], non-decreasing from 0; slots: device int32
+ *       [token_cap]: as ss_block_tables leaves them (a fixed region per unit
+ *       is slots = positions).  A sequence whose first slot is negative, and
+ *       rows behind tok_begin[B], are left out; a block whose page is out of
+ *       range is not written.  A sequence's slots are consecutive places of
+ *       its pages
+ *   open_blocks: device bf16 [B][Hkv][2*blk*d]; rows before the first new
+ *       token's place are read where a block fills; rows of blocks that fill
+ *       in the call, and rows past the last token, are left as they were
+ *   meta: NULL, or the metadata of every block that fills, in meta_kind's
+ *       layout with block capacity nblk_max, from the bf16 keys (the values
+ *       of ss_build_metadata and ss_build_metadata_mean; the mean's fp64 sum
+ *       may run in another order); then positions: device int32 [token_cap].
+ *       Blocks at or above nblk_max get none
+ * Buffers 16-byte aligned.  One launch. */
+ss_status ss_write_kv8(const void *k, const void *v, int64_t tok_stride, int64_t head_stride,
+                       const int32_t *tok_begin, const int32_t *slots, const int32_t *positions, int B, int Hkv, int blk,
+                       int d, int token_cap, int fmt, void *kv_base, const int64_t *region_off, int32_t slot_limit,
+                       void *open_blocks, void *meta, int meta_kind, int nblk_max, void *stream);
+
+/* Reads stored tokens back as bf16 rows (code * scale rounded to fp32, then to
+ * bf16; open tokens as they are), e.g. for the attention of a prompt's next
+ * chunk.  The first row_begin[b+1] - row_begin[b] tokens of sequence b (at
+ * most len[b]) go to output rows row_begin[b] on.
+ *   tables: device int32 [B][max_blocks], or NULL for page j = block j;
+ *   len: device int32 [B]: blocks up to floor(len/blk) are records, the rest
+ *       open rows; row_begin: device int32 [B+1], non-decreasing from 0
+ *   k, v: device bf16, row r of head g at + r*row_stride + g*head_stride
+ *       (bytes, multiples of 16), `rows` rows: none at or past it is written
+ * Blocks whose page is out of range read as zeros.  One launch. */
+ss_status ss_read_kv8(const void *kv_base, const int64_t *region_off, const int32_t *tables, int max_blocks,
+                      int32_t slot_limit, const void *open_blocks, const int32_t *len, const int32_t *row_begin, int B,
+                      int Hkv, int blk, int d, int rows, int fmt, void *k, void *v, int64_t row_stride,
+                      int64_t head_stride, void *stream);
+
+/* ss_sparse_attention over 8-bit records.  Entry i < k of unit u = (b, g) is
+ * block e = sel[u][i], or e = i where sel is NULL (all blocks; nblk is then
+ * needed).  It is skipped if e < 0, or e >= nblk[b] where nblk (device int32
+ * [B]) is given.  Its page is tables[b][e] (skipped if e >= max_blocks) where
+ * tables is given, else e; pages outside [0, slot_limit), or at or above
+ * capacity[u] where that is given, are skipped.  So
+ *   blocks selected from a shared pool: sel, tables, nblk;
+ *   every block of a shared pool: sel NULL, tables, nblk, k = the most blocks;
+ *   slots of an HBM block cache (the slots of ss_cache_resolve): sel, capacity.
+ * open_blocks and len (device int32 [B]; both or neither): the len[b] % blk
+ * tokens of the open record are attended too, in bf16.  With no token the
+ * output is 0.  fp32 accumulation; codes and open tokens enter the products
+ * exactly, probabilities with 24 bits.
+ *   q: device bf16 [B][Hq][d], out: device fp32 [B][Hq][d]
+ *   workspace: device, 4-byte aligned; a smaller one than
+ *   ss_sparse_attention_kv8_workspace (or NULL) is taken with fewer splits
+ *   and another order of the sums
+ * k up to 65536.  Buffers 16-byte aligned. */
+size_t ss_sparse_attention_kv8_workspace(int B, int Hq, int Hkv, int d, int blk, int k);
+ss_status ss_sparse_attention_kv8(const void *q, const void *kv_base, const int64_t *region_off, const int32_t *sel,
+                                  const int32_t *tables, int max_blocks, const int32_t *capacity, int32_t slot_limit,
+                                  const int32_t *nblk, const void *open_blocks, const int32_t *len, int fmt, int B,
+                                  int Hq, int Hkv, int d, int blk, int k, float scale, float *out, void *workspace,
+                                  size_t ws_bytes, void *stream);
+
 /* ------------------------------------------------------ FlashD2H saving
  * CPU-assisted saving of new tokens to the DRAM pool (Section 3.2.2): the
  * contiguous new-KV tensor is copied to pinned host staging memory on the

@@ -102,6 +102,17 @@ _SIGNATURES = {
     "ss_decode_step": (_i32, [_vp, _i32, _i64, _vp, _vp, _vp, _vp, _vp, _vp, _vp]),
     "ss_sparse_attention_static": (_i32, [_vp, _vp, _vp, _vp, _vp, _i32, _i32, _i32, _i32, _i32, _i32, _i32, _f32,
                                           _vp, _vp]),
+    "ss_block_tables": (_i32, [_vp, _vp, _vp, _i32, _i32, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i32,
+                               _vp, _vp, _vp]),
+    "ss_block_release": (_i32, [_vp, _vp, _vp, _i32, _i32, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _vp]),
+    "ss_kv8_record_bytes": (_sz, [_i32, _i32]),
+    "ss_write_kv8": (_i32, [_vp, _vp, _i64, _i64, _vp, _vp, _vp, _i32, _i32, _i32, _i32, _i32, _i32, _vp, _vp, _i32, _vp,
+                            _vp, _i32, _i32, _vp]),
+    "ss_read_kv8": (_i32, [_vp, _vp, _vp, _i32, _i32, _vp, _vp, _vp, _i32, _i32, _i32, _i32, _i32, _i32, _vp, _vp, _i64,
+                           _i64, _vp]),
+    "ss_sparse_attention_kv8_workspace": (_sz, [_i32, _i32, _i32, _i32, _i32, _i32]),
+    "ss_sparse_attention_kv8": (_i32, [_vp, _vp, _vp, _vp, _vp, _i32, _vp, _i32, _vp, _vp, _vp, _i32, _i32, _i32, _i32,
+                                       _i32, _i32, _i32, _f32, _vp, _vp, _sz, _vp]),
 }
 
 
@@ -314,6 +325,53 @@ def ss_append_kv(new_kv, len_dev, nblk_dev, B, Hkv, blk, d, nblk_max, open_block
 
 SS_META_CUBOID, SS_META_MEAN = 0, 1
 SS_AGG_MAX, SS_AGG_SUM = 0, 1
+
+
+SS_KV8_E4M3, SS_KV8_INT8 = 0, 1
+
+
+def ss_block_tables(len_dev, n_new, n_free, B, blk, max_blocks, n_pages, free_pages, tables, len_out, nblk_out,
+                    n_free_out, tok_begin, slots, positions, token_cap, taken, status, stream=None):
+    _check(lib().ss_block_tables(_ptr(len_dev), _ptr(n_new), _ptr(n_free), B, blk, max_blocks, n_pages,
+                                 _ptr(free_pages), _ptr(tables), _ptr(len_out), _ptr(nblk_out), _ptr(n_free_out),
+                                 _ptr(tok_begin), _ptr(slots), _ptr(positions), token_cap, _ptr(taken), _ptr(status),
+                                 _stream(stream)))
+
+
+def ss_block_release(len_dev, done, n_free, B, blk, max_blocks, n_pages, tables, free_pages, len_out, nblk_out,
+                     n_free_out, stream=None):
+    _check(lib().ss_block_release(_ptr(len_dev), _ptr(done), _ptr(n_free), B, blk, max_blocks, n_pages, _ptr(tables),
+                                  _ptr(free_pages), _ptr(len_out), _ptr(nblk_out), _ptr(n_free_out), _stream(stream)))
+
+
+def ss_kv8_record_bytes(blk, d):
+    return int(lib().ss_kv8_record_bytes(blk, d))
+
+
+def ss_write_kv8(k, v, tok_stride, head_stride, tok_begin, slots, positions, B, Hkv, blk, d, token_cap, fmt, kv_base,
+                 region_off, slot_limit, open_blocks, meta=None, meta_kind=0, nblk_max=0, stream=None):
+    _check(lib().ss_write_kv8(_ptr(k), _ptr(v), tok_stride, head_stride, _ptr(tok_begin), _ptr(slots),
+                              _ptr(positions), B, Hkv, blk, d, token_cap, fmt, _ptr(kv_base), _ptr(region_off),
+                              slot_limit, _ptr(open_blocks), _ptr(meta), meta_kind, nblk_max, _stream(stream)))
+
+
+def ss_read_kv8(kv_base, region_off, tables, max_blocks, slot_limit, open_blocks, len_dev, row_begin, B, Hkv, blk, d,
+                rows, fmt, k, v, row_stride, head_stride, stream=None):
+    _check(lib().ss_read_kv8(_ptr(kv_base), _ptr(region_off), _ptr(tables), max_blocks, slot_limit,
+                             _ptr(open_blocks), _ptr(len_dev), _ptr(row_begin), B, Hkv, blk, d, rows, fmt, _ptr(k),
+                             _ptr(v), row_stride, head_stride, _stream(stream)))
+
+
+def ss_sparse_attention_kv8_workspace(B, Hq, Hkv, d, blk, k):
+    return int(lib().ss_sparse_attention_kv8_workspace(B, Hq, Hkv, d, blk, k))
+
+
+def ss_sparse_attention_kv8(q, kv_base, region_off, sel, tables, max_blocks, capacity, slot_limit, nblk, open_blocks,
+                            len_dev, fmt, B, Hq, Hkv, d, blk, k, scale, out, workspace, ws_bytes, stream=None):
+    _check(lib().ss_sparse_attention_kv8(_ptr(q), _ptr(kv_base), _ptr(region_off), _ptr(sel), _ptr(tables), max_blocks,
+                                         _ptr(capacity), slot_limit, _ptr(nblk), _ptr(open_blocks), _ptr(len_dev), fmt,
+                                         B, Hq, Hkv, d, blk, k, float(scale), _ptr(out), _ptr(workspace), ws_bytes,
+                                         _stream(stream)))
 
 
 def ss_build_metadata_mean(kv_base, unit_off, nblk, B, Hkv, nblk_max, blk, d, meta, stream=None):

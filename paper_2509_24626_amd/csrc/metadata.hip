@@ -15,44 +15,21 @@
 // 8 took 15.0 us without them and 16.2 to 18.6 with the non-temporal policy,
 // and the mean keys of 67 MB in blocks of 32 took 12.0 us unit by unit and
 // 13.0 with the heads side by side.
+#include "bf16_keys.hpp"
 #include "internal.hpp"
 
 namespace {
+
+using ss::key2;
+using ss::min2;
+using ss::min_halves;
+using ss::min_rows;
 
 constexpr int D = ss::kHeadDim;
 constexpr int WAVES = 4;
 constexpr int64_t kLargeBytes = 160LL << 20;  // slower at 128 MiB of keys, faster at 192
 
 typedef unsigned int u32x4_t __attribute__((ext_vector_type(4)));
-typedef short i16x2_t __attribute__((ext_vector_type(2)));
-
-// two bf16 values -> two 16-bit keys whose signed order is IEEE totalOrder
-// (-0 < +0): negative values flip their magnitude bits.  Its own inverse.
-__device__ __forceinline__ uint32_t key2(uint32_t w)
-{
-    const i16x2_t sign = __builtin_bit_cast(i16x2_t, w) >> 15;
-    return w ^ (__builtin_bit_cast(uint32_t, sign) & 0x7FFF7FFFu);
-}
-
-__device__ __forceinline__ uint32_t min2(uint32_t a, uint32_t b)
-{
-    return __builtin_bit_cast(uint32_t, __builtin_elementwise_min(__builtin_bit_cast(i16x2_t, a),
-                                                                  __builtin_bit_cast(i16x2_t, b)));
-}
-
-// lanes 0..31: the minimum of a over its two halves, lanes 32..63: that of b
-__device__ __forceinline__ uint32_t min_halves(uint32_t a, uint32_t b)
-{
-    const auto x = __builtin_amdgcn_permlane32_swap(a, b, false, false);
-    return min2(x[0], x[1]);
-}
-
-// per 32 lanes: the first 16 hold the minimum of a over its two 16-lane rows, the others that of b
-__device__ __forceinline__ uint32_t min_rows(uint32_t a, uint32_t b)
-{
-    const auto x = __builtin_amdgcn_permlane16_swap(a, b, false, false);
-    return min2(x[0], x[1]);
-}
 
 template <bool STREAM, class T>
 __device__ __forceinline__ T load(const T *p)

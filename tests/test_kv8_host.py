@@ -1,0 +1,202 @@
+"""The 8-bit KV cache's calls on the CPU: what they refuse, what they launch,
+and the plain implementations that the GPU tests go by."""
+import json
+
+import hip_stand_in
+import kv8_ref as ref
+import numpy as np
+import pytest
+
+from paper_2509_24626_amd import binding as ss
+
+FAKE = 0x1000  # never dereferenced: validation fails first
+
+
+def expect(status, fn, *args):
+    with pytest.raises(ss.SparseServeError) as e:
+        fn(*args)
+    assert e.value.status == status, str(e.value)
+    assert ss.ss_last_error()
+
+
+def tables_args(**kw):
+    a = dict(len=FAKE, n_new=FAKE, n_free=FAKE, B=4, blk=16, max_blocks=8, n_pages=64, free=FAKE, tables=FAKE,
+             len_out=FAKE, nblk_out=None, n_free_out=FAKE, tok_begin=FAKE, slots=FAKE, positions=None, cap=16,
+             taken=FAKE, status=FAKE, stream=0)
+    a.update(kw)
+    return list(a.values())
+
+
+def release_args(**kw):
+    a = dict(len=FAKE, done=FAKE, n_free=FAKE, B=4, blk=16, max_blocks=8, n_pages=64, tables=FAKE, free=FAKE,
+             len_out=FAKE, nblk_out=None, n_free_out=FAKE, stream=0)
+    a.update(kw)
+    return list(a.values())
+
+
+def write_args(**kw):
+    a = dict(k=FAKE, v=FAKE, tok_stride=4096, head_stride=512, tok_begin=FAKE, slots=FAKE, positions=FAKE, B=4, Hkv=8,
+             blk=16, d=128, cap=16, fmt=0, kv=FAKE, region=FAKE, limit=64, open=FAKE, meta=None, kind=0, nblk_max=0,
+             stream=0)
+    a.update(kw)
+    return list(a.values())
+
+
+def read_args(**kw):
+    a = dict(kv=FAKE, region=FAKE, tables=None, max_blocks=0, limit=64, open=FAKE, len=FAKE, begin=FAKE, B=4, Hkv=8,
+             blk=16, d=128, rows=16, fmt=0, k=FAKE, v=FAKE, row_stride=4096, head_stride=512, stream=0)
+    a.update(kw)
+    return list(a.values())
+
+
+def attn_args(**kw):
+    a = dict(q=FAKE, kv=FAKE, region=FAKE, sel=FAKE, tables=None, max_blocks=0, capacity=None, limit=64, nblk=None,
+             open=None, len=None, fmt=0, B=4, Hq=32, Hkv=8, d=128, blk=16, k=16, scale=0.1, out=FAKE, ws=None, bytes=0,
+             stream=0)
+    a.update(kw)
+    return list(a.values())
+
+
+INVALID, UNSUPPORTED = ss.SS_ERR_INVALID_ARG, ss.SS_ERR_UNSUPPORTED
+
+
+@pytest.mark.parametrize("fn, make, kw, status", [
+    ("ss_block_tables", tables_args, dict(B=-1), INVALID),
+    ("ss_block_tables", tables_args, dict(max_blocks=0), INVALID),
+    ("ss_block_tables", tables_args, dict(n_pages=-1), INVALID),
+    ("ss_block_tables", tables_args, dict(cap=-1), INVALID),
+    ("ss_block_tables", tables_args, dict(blk=12), UNSUPPORTED),
+    ("ss_block_tables", tables_args, dict(B=65537), UNSUPPORTED),
+    ("ss_block_tables", tables_args, dict(n_pages=1 << 27), UNSUPPORTED),  # 2^31 slots
+    ("ss_block_tables", tables_args, dict(len=None), INVALID),
+    ("ss_block_tables", tables_args, dict(slots=None), INVALID),
+    ("ss_block_tables", tables_args, dict(status=None), INVALID),
+    ("ss_block_release", release_args, dict(blk=64), UNSUPPORTED),
+    ("ss_block_release", release_args, dict(done=None), INVALID),
+    ("ss_block_release", release_args, dict(max_blocks=-3), INVALID),
+    ("ss_write_kv8", write_args, dict(d=64), UNSUPPORTED),
+    ("ss_write_kv8", write_args, dict(blk=4), UNSUPPORTED),
+    ("ss_write_kv8", write_args, dict(fmt=2), INVALID),
+    ("ss_write_kv8", write_args, dict(Hkv=0), INVALID),
+    ("ss_write_kv8", write_args, dict(tok_stride=4104), INVALID),
+    ("ss_write_kv8", write_args, dict(head_stride=-16), INVALID),
+    ("ss_write_kv8", write_args, dict(limit=-1), INVALID),
+    ("ss_write_kv8", write_args, dict(k=FAKE + 8), INVALID),
+    ("ss_write_kv8", write_args, dict(kv=FAKE + 4), INVALID),
+    ("ss_write_kv8", write_args, dict(open=None), INVALID),
+    ("ss_write_kv8", write_args, dict(meta=FAKE, kind=7), INVALID),
+    ("ss_write_kv8", write_args, dict(meta=FAKE, positions=None), INVALID),
+    ("ss_write_kv8", write_args, dict(meta=FAKE + 8), INVALID),
+    ("ss_write_kv8", write_args, dict(cap=0x7FFFFFF0, Hkv=64, blk=8), UNSUPPORTED),
+    ("ss_read_kv8", read_args, dict(d=256), UNSUPPORTED),
+    ("ss_read_kv8", read_args, dict(rows=-1), INVALID),
+    ("ss_read_kv8", read_args, dict(len=None), INVALID),
+    ("ss_read_kv8", read_args, dict(fmt=-1), INVALID),
+    ("ss_read_kv8", read_args, dict(row_stride=8), INVALID),
+    ("ss_read_kv8", read_args, dict(v=FAKE + 2), INVALID),
+    ("ss_sparse_attention_kv8", attn_args, dict(Hq=30), INVALID),
+    ("ss_sparse_attention_kv8", attn_args, dict(Hq=17, Hkv=1), UNSUPPORTED),
+    ("ss_sparse_attention_kv8", attn_args, dict(d=64), UNSUPPORTED),
+    ("ss_sparse_attention_kv8", attn_args, dict(blk=64), UNSUPPORTED),
+    ("ss_sparse_attention_kv8", attn_args, dict(k=0), INVALID),
+    ("ss_sparse_attention_kv8", attn_args, dict(k=65537), UNSUPPORTED),
+    ("ss_sparse_attention_kv8", attn_args, dict(fmt=3), INVALID),
+    ("ss_sparse_attention_kv8", attn_args, dict(scale=float("inf")), INVALID),
+    ("ss_sparse_attention_kv8", attn_args, dict(sel=None), INVALID),  # all blocks of how many?
+    ("ss_sparse_attention_kv8", attn_args, dict(open=FAKE), INVALID),
+    ("ss_sparse_attention_kv8", attn_args, dict(len=FAKE), INVALID),
+    ("ss_sparse_attention_kv8", attn_args, dict(out=None), INVALID),
+    ("ss_sparse_attention_kv8", attn_args, dict(q=FAKE + 8), INVALID),
+    ("ss_sparse_attention_kv8", attn_args, dict(limit=-1), INVALID),
+])
+def test_refusals(fn, make, kw, status):
+    expect(status, getattr(ss, fn), *make(**kw))
+
+
+def test_empty_work_is_a_no_op():
+    ss.ss_block_tables(*tables_args(B=0, len=None, tables=None))
+    ss.ss_block_release(*release_args(B=0, len=None))
+    ss.ss_write_kv8(*write_args(B=0, k=None))
+    ss.ss_write_kv8(*write_args(cap=0, k=None))
+    ss.ss_read_kv8(*read_args(rows=0, k=None))
+    ss.ss_sparse_attention_kv8(*attn_args(B=0, q=None, sel=None))
+
+
+def test_record_and_workspace_sizes():
+    for blk in (8, 16, 32):
+        assert ss.ss_kv8_record_bytes(blk, 128) == ref.record_bytes(blk)
+    assert ss.ss_kv8_record_bytes(64, 128) == ss.ss_kv8_record_bytes(16, 64) == 0
+    w = ss.ss_sparse_attention_kv8_workspace(1, 32, 8, 128, 16, 4096)
+    assert w > 0 and w % (32 * 130 * 4) == 0
+    assert ss.ss_sparse_attention_kv8_workspace(2, 8, 2, 128, 16, 2) == 0
+    assert ss.ss_sparse_attention_kv8_workspace(1, 30, 8, 128, 16, 64) == 0
+
+
+LAUNCHES = r"""
+P, got = 0x1000, []
+for B, Hq, Hkv, blk, k in json.loads(sys.argv[2]):
+    one = B * Hq * 130 * 4
+    query = ss.ss_sparse_attention_kv8_workspace(B, Hq, Hkv, 128, blk, k)
+    made = []
+    for size in (0, one - 1, one, 2 * one, query // 2, query, 4 * query):
+        ss.ss_sparse_attention_kv8(P, P, P, P, None, 0, None, 64, None, None, None, 0, B, Hq, Hkv, 128, blk, k, 0.1, P,
+                                   P if size else None, size, stream=0)
+        made.append([size, launches()])
+    got.append({"one": one, "query": query, "made": made})
+print(json.dumps(got))
+"""
+
+
+def test_attention_takes_every_workspace_size():
+    """Whatever the workspace, the partials of the launch that it gets fit it."""
+    import tempfile
+    stand_in = hip_stand_in.build(tempfile.mkdtemp()) or pytest.skip("no C compiler")
+    shapes = [(B, hkv * G, hkv, blk, k) for B in (1, 3, 64, 700, 5000) for hkv, G in ((1, 1), (8, 4), (4, 7), (2, 16))
+              for blk, k in ((8, 1), (16, 128), (32, 511), (8, 16384), (32, 65536))]
+    for (B, Hq, Hkv, blk, k), c in zip(shapes, json.loads(hip_stand_in.run(stand_in, LAUNCHES, json.dumps(shapes)))):
+        for size, made in c["made"]:
+            grid = made[0]
+            assert grid[0] == B * Hkv and len(made) == (1 if grid[1] == 1 else 2)
+            if grid[1] > 1:
+                assert grid[1] * c["one"] <= size
+                assert grid[0] * grid[1] <= 4096
+        full = next(m for s, m in c["made"] if s == c["query"])  # the query's size is all that is ever used
+        assert c["made"][-1][1] == full
+        assert c["query"] == (full[0][1] * c["one"] if full[0][1] > 1 else 0)
+
+
+def test_layout_is_a_permutation():
+    for blk in (8, 16, 32):
+        k, v = ref.places(blk)
+        assert sorted(np.concatenate([k.reshape(-1), v.reshape(-1)])) == list(range(2 * blk * 128))
+
+
+@pytest.mark.parametrize("fmt", [0, 1])
+def test_quantisation_in_64_bits(fmt):
+    """The plain quantisation against its definition: a value is off by at
+    most half a step (e4m3: 2^-4 of it, or half of 2^-9 where subnormal), and
+    the products' roundings (2^-22 of the value) besides."""
+    rng = np.random.default_rng(3)
+    x = ref.bf16(rng.standard_normal((40, 16, 128)) * np.exp2(rng.integers(-80, 80, (40, 1, 1))))
+    x[0], x[1, 1:] = 0, 0
+    codes, scale = ref.quantise(x, fmt)
+    back = ref.code_values(fmt)[codes] * scale.astype(np.float64)[:, None, None]
+    step = scale.astype(np.float64)[:, None, None]
+    half = step / 2 if fmt == 1 else np.maximum(np.abs(x) * 2.0 ** -4, step * 2.0 ** -10)
+    assert (np.abs(back - x) <= half + np.abs(x) * 2.0 ** -22).all()
+    assert (np.abs(ref.code_values(fmt)[codes]).max((1, 2))[1:] == ref.Q[fmt]).all()
+    assert (codes[0] == 0).all() and scale[0] == np.float32(2.0 ** -100) / np.float32(ref.Q[fmt])
+
+
+def test_plain_attention_and_its_bound():
+    """The plain attention against one written with sums only, and a planted
+    mistake (one token left out) falls outside the bound."""
+    rng = np.random.default_rng(5)
+    q, k, v = rng.standard_normal((3, 128)), rng.standard_normal((70, 128)), rng.standard_normal((70, 128))
+    out, bound = ref.attention(q, k, v, 1 / np.sqrt(128))
+    for h in range(3):
+        w = [np.exp(sum(q[h] * k[t]) / np.sqrt(128)) for t in range(70)]
+        assert np.allclose(out[h], sum(w[t] * v[t] for t in range(70)) / sum(w), rtol=0, atol=1e-12)
+    less, _ = ref.attention(q, k[:-1], v[:-1], 1 / np.sqrt(128))
+    assert (np.abs(less - out) > bound).any()
+    assert (ref.attention(q, k[:0], v[:0], 1.0)[0] == 0).all()
