@@ -12,7 +12,9 @@
 // One workgroup scans (a thread per sequence, DPP within a wave, the waves'
 // totals through LDS).  Up to kOneGroupRows token rows it also fills the rows
 // itself; beyond, a second launch fills 1024 rows a workgroup, whose lanes
-// find their sequences in the prefix sum.
+// find their sequences in the prefix sums.  Loads that follow one another bound
+// it, so what can be loaded early is: the page of a row's open block and the top
+// of the free list are on their way while the sums run.
 #include <algorithm>
 
 #include "internal.hpp"
@@ -21,9 +23,9 @@ namespace {
 
 constexpr int kMaxSeqs = 65536;
 constexpr int kOneGroupRows = 4096;
-constexpr int kFillRows = 1024;     // rows of a workgroup of the fill kernel
+constexpr int kFillRows = 1024;  // rows of a workgroup of the fill kernel
+constexpr int kSearch = 2048;    // entries of tok_begin that it searches in LDS
 constexpr int kReleasePages = 2048;  // table entries of a workgroup of the release copy
-constexpr int kOneGroupPages = 16384;
 
 typedef int i32x4_t __attribute__((ext_vector_type(4), aligned(4)));
 
@@ -59,22 +61,17 @@ struct row_t {
 };
 
 // One new token of a sequence: its slot, and its page into the table where it
-// is the page's first.  x: the page's number among those the step takes.
-__device__ __forceinline__ row_t place_row(uint32_t pos, uint32_t held, uint32_t taken, int n_free, int n_pages, int shift,
-                                           const int32_t *__restrict__ free_pages, int32_t *table)
+// is the page's first.  page_of(x): the x-th page from the top of the free
+// list; open_page: that of the block in which the tokens held end.
+template <class F>
+__device__ __forceinline__ row_t place_row(uint32_t pos, uint32_t held, uint32_t taken, int open_page, int n_pages, int shift,
+                                           int32_t *table, const F &page_of)
 {
-    const uint32_t j = pos >> shift;
-    int page;
-    if (j >= held) {
-        const int64_t at = (int64_t)n_free - 1 - taken - (j - held);
-        page = at >= 0 ? free_pages[at] : -1;
-        if (page < 0 || page >= n_pages) page = -1;
-        if ((pos & ((1u << shift) - 1)) == 0) table[j] = page;
-    } else {
-        page = table[j];
-        if (page < 0 || page >= n_pages) page = -1;
-    }
-    return {page < 0 ? -1 : (page << shift) + (int)(pos & ((1u << shift) - 1)), (int)pos};
+    const uint32_t j = pos >> shift, place = pos & ((1u << shift) - 1);
+    int page = j >= held ? page_of(taken + (j - held)) : open_page;
+    if (page < 0 || page >= n_pages) page = -1;
+    if (j >= held && place == 0) table[j] = page;
+    return {page < 0 ? -1 : (page << shift) + (int)place, (int)pos};
 }
 
 struct tables_args {
@@ -91,11 +88,13 @@ template <bool FILL>
 __global__ __launch_bounds__(1024) void tables_kernel(const tables_args a)
 {
     __shared__ uint32_t s_rows[16], s_need[16], s_good[16];
+    __shared__ int s_free[FILL ? 1024 : 1];  // the top of the free list, as far as there are threads
     const int t = threadIdx.x, lane = t & 63, waves = blockDim.x >> 6;
     const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
     const uint32_t cap = (uint32_t)a.token_cap;
     int n_free = a.n_free[0];
     n_free = n_free < 0 ? 0 : (n_free > a.n_pages ? a.n_pages : n_free);
+    if (FILL) s_free[t] = t < n_free ? a.free_pages[n_free - 1 - t] : -1;
     uint32_t rows0 = 0, need0 = 0, good0 = 0;  // sums of the chunks before; pages taken so far
     for (int b0 = 0; b0 < a.B; b0 += blockDim.x) {
         const int b = b0 + t;
@@ -106,6 +105,8 @@ __global__ __launch_bounds__(1024) void tables_kernel(const tables_args a)
             n = a.n_new[b];
         }
         const bool bad = len < 0 || n < 0;
+        int open_page = -1;  // of the block that the row's tokens so far end in
+        if (FILL && !bad && live && (len >> a.shift) < a.max_blocks) open_page = a.tables[(int64_t)b * a.max_blocks + (len >> a.shift)];
         const uint32_t nn = n < 0 ? 0u : (uint32_t)n;
         const uint32_t rows = wave_scan(nn);
         if (lane == 63) s_rows[wave] = rows;
@@ -151,11 +152,14 @@ __global__ __launch_bounds__(1024) void tables_kernel(const tables_args a)
             // a lane's own rows one by one where every sequence has few (a decode
             // step), else the wave's sequences in turn, 64 rows at once
             const bool few = !__any(live && nn > 4);
+            auto page_of = [&](uint32_t x) {
+                return x < blockDim.x ? s_free[x] : x < (uint32_t)n_free ? a.free_pages[n_free - 1 - x] : -1;
+            };
             if (few) {
                 int32_t *table = a.tables + (int64_t)b * a.max_blocks;
                 for (uint32_t r = begin; live && r < end; ++r) {
                     row_t x = {-1, -1};
-                    if (st == kServed) x = place_row((uint32_t)len + (r - begin), held, taken, n_free, a.n_pages, a.shift, a.free_pages, table);
+                    if (st == kServed) x = place_row((uint32_t)len + (r - begin), held, taken, open_page, a.n_pages, a.shift, table, page_of);
                     a.slots[r] = x.slot;
                     if (a.positions) a.positions[r] = x.pos;
                 }
@@ -164,11 +168,12 @@ __global__ __launch_bounds__(1024) void tables_kernel(const tables_args a)
                     const int l = __builtin_ctzll(left);
                     const uint32_t len_l = lane_of((uint32_t)len, l), begin_l = lane_of(begin, l), end_l = lane_of(end, l);
                     const uint32_t held_l = lane_of(held, l), taken_l = lane_of(taken, l);
+                    const int open_l = (int)lane_of((uint32_t)open_page, l);
                     const bool served = lane_of((uint32_t)st, l) == kServed;
                     int32_t *table = a.tables + (int64_t)(b0 + wave * 64 + l) * a.max_blocks;
                     for (uint32_t r = begin_l + lane; r < end_l; r += 64) {
                         row_t x = {-1, -1};
-                        if (served) x = place_row(len_l + (r - begin_l), held_l, taken_l, n_free, a.n_pages, a.shift, a.free_pages, table);
+                        if (served) x = place_row(len_l + (r - begin_l), held_l, taken_l, open_l, a.n_pages, a.shift, table, page_of);
                         a.slots[r] = x.slot;
                         if (a.positions) a.positions[r] = x.pos;
                     }
@@ -192,61 +197,97 @@ __global__ __launch_bounds__(1024) void tables_kernel(const tables_args a)
         }
 }
 
-// the last of the sequences [0, n) that begins at or before row r (tok_begin[0] is 0): 64 probes a round
-__device__ __forceinline__ int find_seq(const int32_t *__restrict__ tok_begin, int n, uint32_t r, int lane)
-{
-    int lo = 0;
-    for (int span = n; span > 1;) {
-        const int step = (span + 63) / 64, b = lo + lane * step;
-        const unsigned long long at = __ballot(b < n && (uint32_t)tok_begin[b < n ? b : n - 1] <= r);
-        lo += (at ? 63 - __builtin_clzll(at) : 0) * step;
-        span = step;
-    }
-    return lo;
-}
+struct seq_t {
+    uint32_t len, held, taken;  // tokens and pages before the step, pages taken before the sequence
+    bool served;
+};
 
 // Rows of large batches: what the scan left in tok_begin, taken, status,
-// len_out and n_free_out says everything else.
+// len_out and n_free_out says everything else.  The row's sequence is found in
+// a copy of tok_begin in LDS (of every `step`-th entry where there are more
+// than fit, the rest from memory), so that three loads follow one another:
+// tok_begin, the sequence, the page.
 __global__ __launch_bounds__(256) void fill_rows_kernel(const tables_args a)
 {
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    __shared__ uint32_t s_begin[kSearch];
     const uint32_t cap = (uint32_t)a.token_cap, total = (uint32_t)a.tok_begin[a.B];
-    const uint32_t base = (uint32_t)blockIdx.x * kFillRows + wave * 256;
-    if (base >= cap) return;
     const int n_free = a.n_free_out[0] + a.taken[a.B];
-    int b = 0, last = 0;
-    if (base < total) {
-        b = find_seq(a.tok_begin, a.B, base, lane);
-        last = find_seq(a.tok_begin, a.B, min(base + 255, total - 1), lane);
+    const int step = (a.B + kSearch - 1) / kSearch, n = (a.B + step - 1) / step;
+    for (int i = threadIdx.x; i < n; i += 256) s_begin[i] = (uint32_t)a.tok_begin[i * step];
+    __syncthreads();
+    const uint32_t r0 = (uint32_t)blockIdx.x * kFillRows + threadIdx.x * 4;
+    // the last sequence that begins at or before a row (tok_begin[0] is 0): for
+    // the wave's first row and its last together, 64 probes at once; only
+    // where they differ does a lane look for its own
+    const int lane = threadIdx.x & 63;
+    const uint32_t w0 = (uint32_t)blockIdx.x * kFillRows + (threadIdx.x - lane) * 4;
+    auto last_of = [](unsigned long long at) { return at ? 63 - __builtin_clzll(at) : 0; };
+    constexpr int kCoarse = kSearch / 64;
+    const int i0 = lane * kCoarse;
+    const uint32_t x = i0 < n ? s_begin[i0] : ~0u;
+    const int lo0 = last_of(__ballot(x <= w0)) * kCoarse, hi0 = last_of(__ballot(x <= w0 + 255)) * kCoarse;
+    const uint32_t y = lane < kCoarse && lo0 + lane < n ? s_begin[lo0 + lane] : ~0u;
+    const uint32_t z = lane < kCoarse && hi0 + lane < n ? s_begin[hi0 + lane] : ~0u;
+    int b = lo0 + last_of(__ballot(y <= w0));
+    for (int hi = hi0 + last_of(__ballot(z <= w0 + 255)); b < hi;) {
+        const int mid = (b + hi + 1) >> 1;
+        if (s_begin[mid] <= r0) b = mid;
+        else hi = mid - 1;
     }
-    const uint32_t r0 = base + lane * 4;
-    // this lane's first sequence, in [b, last]
-    for (int hi = last; b < hi;) {
+    b *= step;
+    for (int hi = min(b + step, a.B) - 1; b < hi;) {
         const int mid = (b + hi + 1) >> 1;
         if ((uint32_t)a.tok_begin[mid] <= r0) b = mid;
         else hi = mid - 1;
     }
+    if (r0 >= cap) return;
+    auto page_of = [&](uint32_t i) { return i < (uint32_t)n_free ? a.free_pages[n_free - 1 - i] : -1; };
     i32x4_t slot = {-1, -1, -1, -1}, pos = {-1, -1, -1, -1};
-    int of = -1;  // the sequence whose values follow
-    uint32_t begin = 0, end = 0, len = 0, held = 0, taken = 0;
-    bool served = false;
+    uint32_t begin = 0, end = 0;
+    seq_t q = {};
+    int32_t *table = nullptr;
+    auto enter = [&] {  // sequence b
+        begin = (uint32_t)a.tok_begin[b];
+        end = (uint32_t)a.tok_begin[b + 1];
+        const uint32_t len = (uint32_t)a.len_out[b];
+        const uint32_t taken = (uint32_t)a.taken[b];
+        q.served = a.status[b] == kServed;
+        q.len = len - (end - begin);
+        q.held = blocks_of(q.len, a.shift);
+        q.taken = taken;
+        table = a.tables + (int64_t)b * a.max_blocks;
+    };
+    enter();
+    if (r0 + 4 <= end && r0 >= begin) {
+        // four rows of one sequence, as most are: they lie in one block or two
+        if (q.served) {
+            const uint32_t p0 = q.len + (r0 - begin), mask = (1u << a.shift) - 1;
+            const uint32_t j0 = p0 >> a.shift, j1 = (p0 + 3) >> a.shift;
+            int first = j0 >= q.held ? page_of(q.taken + (j0 - q.held)) : table[j0];
+            int second = j1 >= q.held ? page_of(q.taken + (j1 - q.held)) : table[j1];
+            if (first < 0 || first >= a.n_pages) first = -1;
+            if (second < 0 || second >= a.n_pages) second = -1;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const uint32_t r = r0 + i;
-        if (r >= total) break;
-        while (b < last && (uint32_t)a.tok_begin[b + 1] <= r) ++b;
-        if (b != of) {
-            of = b;
-            begin = (uint32_t)a.tok_begin[b];
-            end = (uint32_t)a.tok_begin[b + 1];
-            served = a.status[b] == kServed;
-            len = (uint32_t)a.len_out[b] - (end - begin);
-            held = blocks_of(len, a.shift);
-            taken = (uint32_t)a.taken[b];
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t p = p0 + i, j = p >> a.shift;
+                const int page = j == j0 ? first : second;
+                slot[i] = page < 0 ? -1 : (page << a.shift) + (int)(p & mask);
+                pos[i] = (int)p;
+                if ((p & mask) == 0 && j >= q.held) table[j] = page;
+            }
         }
-        if (served) {
-            const row_t x = place_row(len + (r - begin), held, taken, n_free, a.n_pages, a.shift, a.free_pages,
-                                      a.tables + (int64_t)b * a.max_blocks);
+    } else {
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t r = r0 + i;
+            if (r >= total) break;
+            while (r >= end) {
+                ++b;
+                enter();
+            }
+            if (!q.served) continue;
+            const uint32_t at = q.len + (r - begin);
+            const int open_page = (at >> a.shift) < q.held ? table[at >> a.shift] : -1;
+            const row_t x = place_row(at, q.held, q.taken, open_page, a.n_pages, a.shift, table, page_of);
             slot[i] = x.slot;
             pos[i] = x.pos;
         }
@@ -272,9 +313,8 @@ struct release_args {
 // pages that sequence b gives back
 __device__ __forceinline__ uint32_t gives_back(const release_args &a, int b)
 {
-    if (!a.done[b]) return 0;
-    const int n = a.len[b];
-    return n <= 0 ? 0u : min(blocks_of((uint32_t)n, a.shift), (uint32_t)a.max_blocks);
+    const int done = a.done[b], n = a.len[b];  // neither load waits for the other
+    return done && n > 0 ? min(blocks_of((uint32_t)n, a.shift), (uint32_t)a.max_blocks) : 0u;
 }
 
 __device__ __forceinline__ uint32_t block_sum(uint32_t x, uint32_t *s_part)
@@ -288,68 +328,63 @@ __device__ __forceinline__ uint32_t block_sum(uint32_t x, uint32_t *s_part)
     return sum;
 }
 
-// Entries of one finished sequence's row onto the free list, behind those of
-// the finished sequences before it.
-__device__ __forceinline__ void push_row(const release_args &a, int b, uint32_t from, uint32_t to, int64_t at)
+__device__ __forceinline__ uint32_t sum_before(const release_args &a, int n, uint32_t *s_part)
 {
-    const int32_t *row = a.tables + (int64_t)b * a.max_blocks;
-    for (uint32_t j = from + threadIdx.x; j < to; j += blockDim.x) {
-        const int page = row[j];
-        if (at + j < a.n_pages) a.free_pages[at + j] = page < 0 || page >= a.n_pages ? -1 : page;
-    }
+    uint32_t sum = 0;
+    for (int i = threadIdx.x; i < n; i += blockDim.x) sum = add_sat(sum, gives_back(a, i));
+    return block_sum(sum, s_part);
 }
 
-__device__ __forceinline__ int clamp_free(const release_args &a)
+__device__ __forceinline__ void put_lengths(const release_args &a, int from, int stride)
 {
-    const int n = a.n_free[0];
-    return n < 0 ? 0 : (n > a.n_pages ? a.n_pages : n);
-}
-
-// A workgroup copies up to kReleasePages entries of a row; most find a row
-// that is not done, or shorter, and leave.  Each sums what the sequences
-// before give back itself, so that the copy needs nothing from another launch.
-__global__ __launch_bounds__(256) void release_copy_kernel(const release_args a, int chunks)
-{
-    __shared__ uint32_t s_part[4];
-    for (int64_t w = blockIdx.x; w < (int64_t)a.B * chunks; w += gridDim.x) {
-        const int b = (int)(w / chunks);
-        const uint32_t from = (uint32_t)(w - (int64_t)b * chunks) * kReleasePages, count = gives_back(a, b);
-        if (from >= count) continue;
-        uint32_t sum = 0;
-        for (int i = threadIdx.x; i < b; i += 256) sum = add_sat(sum, gives_back(a, i));
-        const uint32_t before = block_sum(sum, s_part);
-        push_row(a, b, from, min(count, from + kReleasePages), (int64_t)clamp_free(a) + before);
-    }
-}
-
-// COPY: the entries too, row after row (small tables)
-template <bool COPY>
-__global__ __launch_bounds__(1024) void release_kernel(const release_args a)
-{
-    __shared__ uint32_t s_part[16];
-    const int n_free = clamp_free(a);
-    uint32_t total = 0;
-    if (COPY) {
-        const int lane = threadIdx.x & 63;  // a sequence each
-        const uint32_t count = lane < a.B ? gives_back(a, lane) : 0u, upto = wave_scan(count);
-        for (unsigned long long left = __ballot(count > 0); left; left &= left - 1) {
-            const int b = __builtin_ctzll(left);
-            const uint32_t n = lane_of(count, b);
-            push_row(a, b, 0, n, (int64_t)n_free + (lane_of(upto, b) - n));
-        }
-        total = lane_of(upto, 63);
-        __syncthreads();  // every wave has read the lengths
-    } else {
-        uint32_t sum = 0;
-        for (int b = threadIdx.x; b < a.B; b += blockDim.x) sum = add_sat(sum, gives_back(a, b));
-        total = block_sum(sum, s_part);
-    }
-    for (int b = threadIdx.x; b < a.B; b += blockDim.x) {
+    for (int b = from; b < a.B; b += stride) {
         const int n = a.done[b] ? 0 : a.len[b];
         a.len_out[b] = n;
         if (a.nblk_out) a.nblk_out[b] = n < 0 ? 0 : n >> a.shift;
     }
-    if (threadIdx.x == 0) a.n_free_out[0] = (int)min((int64_t)n_free + total, (int64_t)a.n_pages);
+}
+
+// A workgroup copies up to kReleasePages entries of a row behind those of the
+// finished rows before it; most find a row that is not done, or shorter, and
+// go on.  Each sums what the rows before give back itself, so that the copy
+// needs nothing from another launch.  LENGTHS: the lengths and the count too,
+// where they are written apart from what is read.
+template <bool LENGTHS>
+__global__ __launch_bounds__(256) void release_kernel(const release_args a, int chunks)
+{
+    __shared__ uint32_t s_part[4];
+    int n_free = a.n_free[0];
+    n_free = n_free < 0 ? 0 : (n_free > a.n_pages ? a.n_pages : n_free);
+    for (int64_t w = blockIdx.x; w < (int64_t)a.B * chunks; w += gridDim.x) {
+        const int b = (int)(w / chunks);
+        const uint32_t from = (uint32_t)(w - (int64_t)b * chunks) * kReleasePages, count = gives_back(a, b);
+        if (from >= count) continue;
+        const int64_t at = (int64_t)n_free + sum_before(a, b, s_part);
+        const int32_t *row = a.tables + (int64_t)b * a.max_blocks;
+        const uint32_t to = min(count, from + kReleasePages);
+        for (uint32_t j = from + threadIdx.x; j < to; j += 256) {
+            const int page = row[j];
+            if (at + j < a.n_pages) a.free_pages[at + j] = page < 0 || page >= a.n_pages ? -1 : page;
+        }
+    }
+    if (LENGTHS) {
+        put_lengths(a, blockIdx.x * 256 + threadIdx.x, gridDim.x * 256);
+        if (blockIdx.x == gridDim.x - 1) {
+            const int64_t all = (int64_t)n_free + sum_before(a, a.B, s_part);
+            if (threadIdx.x == 0) a.n_free_out[0] = (int)min(all, (int64_t)a.n_pages);
+        }
+    }
+}
+
+// the lengths and the count where they are updated in place
+__global__ __launch_bounds__(1024) void release_lengths_kernel(const release_args a)
+{
+    __shared__ uint32_t s_part[16];
+    int n_free = a.n_free[0];
+    n_free = n_free < 0 ? 0 : (n_free > a.n_pages ? a.n_pages : n_free);
+    const int64_t all = (int64_t)n_free + sum_before(a, a.B, s_part);
+    put_lengths(a, threadIdx.x, blockDim.x);
+    if (threadIdx.x == 0) a.n_free_out[0] = (int)min(all, (int64_t)a.n_pages);
 }
 
 int shift_of(int blk) { return blk == 8 ? 3 : blk == 16 ? 4 : 5; }
@@ -403,15 +438,12 @@ extern "C" ss_status ss_block_release(const int32_t *len, const int32_t *done, c
     const release_args a = {len, done, n_free, B, shift_of(blk), max_blocks, n_pages, tables, free_pages, len_out,
                             nblk_out, n_free_out};
     hipStream_t s = ss::as_stream(stream);
-    if ((int64_t)B * max_blocks <= kOneGroupPages && B <= 64) {
-        ss::launch(release_kernel<true>, dim3(1), dim3(1024), s, a);
-        return ss::check_launch("ss_block_release");
-    }
-    const int chunks = (int)std::min<int64_t>(((int64_t)max_blocks + kReleasePages - 1) / kReleasePages, kMaxSeqs);
+    const int chunks = (max_blocks - 1) / kReleasePages + 1;
     const int64_t groups = std::min<int64_t>((int64_t)B * chunks, 4096);
-    ss::launch(release_copy_kernel, dim3((unsigned)groups), dim3(256), s, a, chunks);
+    const bool apart = len_out != len && n_free_out != n_free;
+    ss::launch(apart ? release_kernel<true> : release_kernel<false>, dim3((unsigned)groups), dim3(256), s, a, chunks);
     st = ss::check_launch("ss_block_release");
-    if (st) return st;
-    release_kernel<false><<<dim3(1), dim3(1024), 0, s>>>(a);
+    if (st != SS_OK || apart) return st;
+    release_lengths_kernel<<<dim3(1), dim3(1024), 0, s>>>(a);
     return ss::check_launch("ss_block_release(lengths)");
 }

@@ -95,7 +95,8 @@ class Tables:
 
 @pytest.mark.parametrize("B, blk, longest, in_place", [
     (1, 16, 3, True), (1, 8, 9000, False), (2, 32, 5000, True), (63, 16, 40, True), (64, 8, 1, False),
-    (65, 32, 700, True), (200, 16, 90, False), (1000, 8, 12, True), (1025, 16, 3, True), (1500, 8, 30, False)])
+    (65, 32, 700, True), (200, 16, 90, False), (1000, 8, 12, True), (1025, 16, 3, True), (1500, 8, 30, False),
+    (4100, 8, 40, True), (9000, 16, 5, False)])
 def test_tables_over_several_steps(ss, B, blk, longest, in_place):
     """Rows that join, grow, idle and finish over five steps of every length
     up to `longest`, with one launch (up to 4096 token rows) and with two."""
