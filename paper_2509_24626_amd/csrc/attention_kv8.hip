@@ -44,6 +44,20 @@ typedef unsigned int u32x2_t __attribute__((ext_vector_type(2)));
 typedef float f32x2_t __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
 
+// Records are addressed as global memory explicitly: where the compiler lost
+// that, it would wait for all loads in flight, the next step's among them.
+typedef const uint8_t __attribute__((address_space(1))) *gptr_t;
+template <class T>
+__device__ __forceinline__ T load_stream(gptr_t p)
+{
+    return __builtin_nontemporal_load(reinterpret_cast<const T __attribute__((address_space(1))) *>(p));
+}
+template <class T>
+__device__ __forceinline__ T load(gptr_t p)
+{
+    return *reinterpret_cast<const T __attribute__((address_space(1))) *>(p);
+}
+
 // what a skipped entry reads
 __device__ __align__(128) unsigned char zero_record[ss::kv8_record(32)];
 
@@ -75,6 +89,22 @@ __device__ __forceinline__ float rows_max(float x)
     const auto h = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
     return fmaxf(__uint_as_float(h[0]), __uint_as_float(h[1]));
 }
+
+// over all lanes, in every lane and in a fixed order
+template <class F>
+__device__ __forceinline__ float wave_fold(float x, const F &f)
+{
+    x = f(x, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), 0xB1, 0xF, 0xF, false)));   // lane ^ 1
+    x = f(x, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), 0x4E, 0xF, 0xF, false)));   // lane ^ 2
+    x = f(x, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), 0x141, 0xF, 0xF, false)));  // mirrored in 8 lanes
+    x = f(x, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), 0x140, 0xF, 0xF, false)));  // mirrored in 16 lanes
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = f(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    const auto h = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return f(__uint_as_float(h[0]), __uint_as_float(h[1]));
+}
+__device__ __forceinline__ float wave_max(float x) { return wave_fold(x, [](float a, float b) { return fmaxf(a, b); }); }
+__device__ __forceinline__ float wave_sum(float x) { return wave_fold(x, [](float a, float b) { return a + b; }); }
 
 struct attn_args {
     const uint16_t *q;
@@ -139,21 +169,20 @@ __global__ __launch_bounds__(WAVES * 64, 3) void attn_kv8_kernel(const attn_args
         qf[m].u = col < a.G ? w : u32x4_t{0, 0, 0, 0};
     }
 
-    const uint8_t *base = a.kv + a.region_off[u];
+    const gptr_t base = (gptr_t)(a.kv + a.region_off[u]);
     int limit = a.slot_limit;
     if (a.capacity) limit = min(limit, a.capacity[u]);
     const int blocks = a.nblk ? a.nblk[b] : 0x7FFFFFFF;
-    // the page of entry i of the wave's steps from step `first` on, a lane each
+    // the page of entry i of the wave's steps from step `first` on, a lane each.
+    // What bounds an entry by the sequence's length is applied last, so that no
+    // load waits for the length.
     auto resolve = [&](int first) {
         const int st = first + (lane / EPS) * WAVES, e = st * EPS + lane % EPS;
-        int page = -1;
-        if (st < s_end && e < n_entries) {
-            page = a.sel ? a.sel[(int64_t)u * a.k + e] : e;
-            if (page >= blocks) page = -1;
-            if (a.tables && page >= 0) page = page < a.max_blocks ? a.tables[(int64_t)b * a.max_blocks + page] : -1;
-            if (page >= limit) page = -1;
-        }
-        return page;
+        int block = -1, page = -1;
+        if (e < a.k) block = a.sel ? a.sel[(int64_t)u * a.k + e] : e;
+        if (!a.tables) page = block;
+        else if (block >= 0 && block < a.max_blocks) page = a.tables[(int64_t)b * a.max_blocks + block];
+        return st < s_end && e < n_entries && block < blocks && page < limit ? page : -1;
     };
 
     float mrun = -INFINITY, lrun = 0.f;
@@ -168,7 +197,7 @@ __global__ __launch_bounds__(WAVES * 64, 3) void attn_kv8_kernel(const attn_args
         cm = rows_max(cm);
         const float mnew = fmaxf(mrun, cm);
         const float m0 = mnew == -INFINITY ? 0.f : mnew;  // nothing yet: every p is 0
-        if (__any(mnew != mrun)) {
+        if (__builtin_expect(__any(mnew != mrun), 0)) {
             const float alpha = __builtin_amdgcn_exp2f(mrun - m0);
 #pragma unroll
             for (int t = 0; t < 8; ++t) o[t] *= alpha;
@@ -197,65 +226,81 @@ __global__ __launch_bounds__(WAVES * 64, 3) void attn_kv8_kernel(const attn_args
             drop(p2.w[i >> 1]);
             p3.w[i >> 1] = upper();
         }
+        // four accumulators in turn, so that none waits for its last product
 #pragma unroll
-        for (int t = 0; t < 8; ++t) {
-            const frag_t v = vfrag(t);
-            o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v.v, p1.v, o[t], 0, 0, 0);
-            o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v.v, p2.v, o[t], 0, 0, 0);
-            o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v.v, p3.v, o[t], 0, 0, 0);
+        for (int t = 0; t < 8; t += 4) {
+            frag_t v[4];
+#pragma unroll
+            for (int h = 0; h < 4; ++h) v[h] = vfrag(t + h);
+#pragma unroll
+            for (int h = 0; h < 4; ++h) o[t + h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[h].v, p1.v, o[t + h], 0, 0, 0);
+#pragma unroll
+            for (int h = 0; h < 4; ++h) o[t + h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[h].v, p2.v, o[t + h], 0, 0, 0);
+#pragma unroll
+            for (int h = 0; h < 4; ++h) o[t + h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[h].v, p3.v, o[t + h], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
         }
     };
 
+    gptr_t zeros = (gptr_t)zero_record;
+    asm("" : "+s"(zeros));  // its address is looked up once
     struct step_t {
         u32x4_t k[4], v[4];  // subtile 0, 1; channels 0..63, 64..127 (K), channel quads (V)
         f32x2_t sc[2];       // scales of the lane's accumulator tokens
         bool ok[2];
     };
     auto load_step = [&](const int (&page)[EPS], step_t &x) {
-        const uint8_t *rec[EPS];
+        gptr_t rec[EPS];
 #pragma unroll
-        for (int e = 0; e < EPS; ++e) rec[e] = page[e] >= 0 ? base + (int64_t)page[e] * REC : zero_record;
-        auto get = [](const uint8_t *p) { return __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(p)); };
+        for (int e = 0; e < EPS; ++e) {
+            // both addresses first: a branch would hold the loads back
+            gptr_t r = base + (int64_t)page[e] * REC;
+            asm("" : "+s"(r));
+            rec[e] = page[e] >= 0 ? r : zeros;
+        }
+        auto get = [](gptr_t p) { return load_stream<u32x4_t>(p); };
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
             if constexpr (BLK == 8) {
                 const bool kw = col >> 3, vw = L >> 1;  // which of the subtile's two records
-                const uint8_t *kr = (kw ? rec[2 * s + 1] : rec[2 * s]) + L * 128 + (col & 7) * 16;
-                const uint8_t *r = vw ? rec[2 * s + 1] : rec[2 * s];
-                const uint8_t *vr = r + BLK * D + (L & 1) * 256 + col * 16;
+                const gptr_t kr = (kw ? rec[2 * s + 1] : rec[2 * s]) + L * 128 + (col & 7) * 16;
+                const gptr_t r = vw ? rec[2 * s + 1] : rec[2 * s];
+                const gptr_t vr = r + BLK * D + (L & 1) * 256 + col * 16;
                 x.k[2 * s] = get(kr);
                 x.k[2 * s + 1] = get(kr + 512);
                 x.v[2 * s] = get(vr);
                 x.v[2 * s + 1] = get(vr + 512);
-                x.sc[s] = *reinterpret_cast<const f32x2_t *>(r + 2 * BLK * D);
+                x.sc[s] = load<f32x2_t>(r + 2 * BLK * D);
                 x.ok[s] = (vw ? page[2 * s + 1] : page[2 * s]) >= 0;
             } else {
                 constexpr int PER = BLK / 16;  // subtiles of a record
-                const uint8_t *r = rec[s / PER] + lane * 16;
+                const gptr_t r = rec[s / PER] + lane * 16;
                 x.k[2 * s] = get(r + (s % PER) * 2048);
                 x.k[2 * s + 1] = get(r + (s % PER) * 2048 + 1024);
                 x.v[2 * s] = get(r + BLK * D + (s % PER) * 2048);
                 x.v[2 * s + 1] = get(r + BLK * D + (s % PER) * 2048 + 1024);
-                x.sc[s] = *reinterpret_cast<const f32x2_t *>(rec[s / PER] + 2 * BLK * D);
+                x.sc[s] = load<f32x2_t>(rec[s / PER] + 2 * BLK * D);
                 x.ok[s] = page[s / PER] >= 0;
             }
         }
     };
     auto compute_step = [&](const step_t &x) {
         float z[8];
+        f32x4_t acc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
+        for (int m = 0; m < 4; ++m)
 #pragma unroll
-            for (int m = 0; m < 4; ++m) {
+            for (int s = 0; s < 2; ++s) {
                 frag_t f;
                 widen4<FMT>(x.k[2 * s + (m >> 1)][2 * (m & 1)], f.w[0], f.w[1]);
                 widen4<FMT>(x.k[2 * s + (m >> 1)][2 * (m & 1) + 1], f.w[2], f.w[3]);
-                acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f.v, qf[m].v, acc, 0, 0, 0);
+                acc[s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f.v, qf[m].v, acc[s], 0, 0, 0);
             }
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
             const float sk = x.sc[s].x * a.scale_log2;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) z[4 * s + i] = x.ok[s] ? acc[i] * sk : -INFINITY;
+            for (int i = 0; i < 4; ++i) z[4 * s + i] = x.ok[s] ? acc[s][i] * sk : -INFINITY;
         }
         attend(z, x.sc[0].y, x.sc[1].y, [&](int t) {
             frag_t f;
@@ -273,7 +318,7 @@ __global__ __launch_bounds__(WAVES * 64, 3) void attn_kv8_kernel(const attn_args
 #pragma unroll
         for (int e = 0; e < EPS; ++e) page[e] = __builtin_amdgcn_readlane(pages, at * EPS + e);
         load_step(page, x);
-        if (++at == SET) {
+        if (__builtin_expect(++at == SET, 0)) {
             at = 0;
             pages = ahead;
             ahead = resolve(later);
@@ -368,50 +413,63 @@ __global__ __launch_bounds__(WAVES * 64, 3) void attn_kv8_kernel(const attn_args
     }
 }
 
-// Merges a unit's splits in their order, one workgroup per (unit, head): each
-// wave takes a run of splits, two channels a lane, and the waves' sums are
-// merged through LDS.  A split without a token has the maximum -inf and is
-// not read further.
-constexpr int CW = 4;  // waves
-
-__global__ __launch_bounds__(CW * 64) void combine_kv8_kernel(const float *__restrict__ ws, int Hq, int Hkv, int G,
-                                                              int splits, float *__restrict__ out)
+// Merges a unit's splits in their order, one workgroup per (unit, head), two
+// channels a lane.  Each of the W waves takes up to N splits, whose partials
+// it reads at once, beside all splits' maxima and sums (a split a lane): no
+// load waits for another.  A split without a token has the maximum -inf and
+// no partial.
+template <int W, int N>
+__global__ __launch_bounds__(W * 64) void combine_kv8_kernel(const float *__restrict__ ws, int Hq, int Hkv, int G,
+                                                             int splits, float *__restrict__ out)
 {
-    __shared__ float s_l[CW];
-    __shared__ f32x2_t s_o[CW][64];
+    constexpr int PER = (W * N + 63) / 64;  // splits of a lane
+    typedef float f2_t __attribute__((ext_vector_type(2), aligned(4)));
+    __shared__ f32x2_t s_o[W][64];
     const int u = blockIdx.x, h = blockIdx.y, lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const float *p = ws + ((int64_t)u * splits * G + h) * (D + 2);
     const int64_t stride = (int64_t)G * (D + 2);
-    float M = -INFINITY;
-    for (int s = lane; s < splits; s += 64) M = fmaxf(M, p[s * stride]);
+    const float *p = ws + (int64_t)u * splits * stride + h * (D + 2);
+    f2_t x[N];
 #pragma unroll
-    for (int x = 1; x < 64; x <<= 1) M = fmaxf(M, __shfl_xor(M, x));
-    const float m0 = M == -INFINITY ? 0.f : M;
-    const int per = (splits + CW - 1) / CW, s1 = min((wave + 1) * per, splits);
-    float lsum = 0.f;
-    f32x2_t osum = {0.f, 0.f};
-    typedef float f2_t __attribute__((ext_vector_type(2), aligned(4)));
-#pragma unroll 4
-    for (int s = wave * per; s < s1; ++s) {
-        const float m = p[s * stride];
-        if (m == -INFINITY) continue;
-        const float w = __builtin_amdgcn_exp2f(m - m0);
-        lsum += w * p[s * stride + 1];
-        const f2_t x = *reinterpret_cast<const f2_t *>(p + s * stride + 2 + 2 * lane);
-        osum.x += w * x.x;
-        osum.y += w * x.y;
+    for (int i = 0; i < N; ++i) x[i] = *reinterpret_cast<const f2_t *>(p + min(wave * N + i, splits - 1) * stride + 2 + 2 * lane);
+    f2_t ml[PER];
+    float M = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        ml[i] = f2_t{-INFINITY, 0.f};
+        if (i * 64 + lane < splits) ml[i] = *reinterpret_cast<const f2_t *>(p + (i * 64 + lane) * stride);
+        M = fmaxf(M, ml[i].x);
     }
-    if (lane == 0) s_l[wave] = lsum;
-    s_o[wave][lane] = osum;
-    __syncthreads();
+    M = wave_max(M);
+    const float m0 = M == -INFINITY ? 0.f : M;
+    float w[PER], lsum = 0.f;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        w[i] = __builtin_amdgcn_exp2f(ml[i].x - m0);
+        lsum += ml[i].x == -INFINITY ? 0.f : w[i] * ml[i].y;
+    }
+    f32x2_t osum = {0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int s = wave * N + i;  // its weight: lane s % 64 of the s / 64-th
+        float own = w[0];
+#pragma unroll
+        for (int j = 1; j < PER; ++j) own = s / 64 == j ? w[j] : own;
+        const float sc = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(own), s % 64));
+        if (s < splits && sc != 0.f) {
+            osum.x += sc * x[i].x;
+            osum.y += sc * x[i].y;
+        }
+    }
+    if (wave) s_o[wave][lane] = osum;
+    if (W > 1) __syncthreads();
     if (wave) return;
 #pragma unroll
-    for (int w = 1; w < CW; ++w) {
-        lsum += s_l[w];
-        osum.x += s_o[w][lane].x;
-        osum.y += s_o[w][lane].y;
+    for (int j = 1; j < W; ++j) {
+        osum.x += s_o[j][lane].x;
+        osum.y += s_o[j][lane].y;
     }
+    lsum = wave_sum(lsum);
     f2_t y = {0.f, 0.f};
     if (lsum != 0.f) y = f2_t{osum.x / lsum, osum.y / lsum};
     const int b = u / Hkv, g = u - b * Hkv;
@@ -491,6 +549,15 @@ extern "C" ss_status ss_sparse_attention_kv8(const void *q, const void *kv_base,
                dim3(WAVES * 64), s, a);
     ss_status st = ss::check_launch("ss_sparse_attention_kv8");
     if (st != SS_OK || sp.splits == 1) return st;
-    combine_kv8_kernel<<<dim3((unsigned)units, G), dim3(CW * 64), 0, s>>>(a.ws, Hq, Hkv, G, sp.splits, out);
+    // reads as many partials as there may be splits
+    auto *combine = combine_kv8_kernel<16, 16>;
+    int waves = 16;
+    if (sp.splits <= 4) combine = combine_kv8_kernel<1, 4>, waves = 1;
+    else if (sp.splits <= 8) combine = combine_kv8_kernel<1, 8>, waves = 1;
+    else if (sp.splits <= 16) combine = combine_kv8_kernel<2, 8>, waves = 2;
+    else if (sp.splits <= 32) combine = combine_kv8_kernel<4, 8>, waves = 4;
+    else if (sp.splits <= 64) combine = combine_kv8_kernel<8, 8>, waves = 8;
+    else if (sp.splits <= 128) combine = combine_kv8_kernel<16, 8>, waves = 16;
+    combine<<<dim3((unsigned)units, G), dim3(waves * 64), 0, s>>>(a.ws, Hq, Hkv, G, sp.splits, out);
     return ss::check_launch("ss_sparse_attention_kv8(merge)");
 }
