@@ -9,7 +9,7 @@
 // e4m3 and int8 codes are exact in bf16, so they are widened in registers and
 // the tiles' scales go where they cost one multiplication a token: K's into
 // the logit, V's into the probability.  P then enters the product as three
-// bf16 parts (24 bits; two lose the last 8 and showed as 1e-5 in the output).
+// bf16 parts, 8 bits each, which keep all 24 of it.
 // The record's order of codes (kv8.hpp) makes a load instruction 1 KiB of
 // consecutive bytes and leaves each lane with its own operand bytes, so
 // nothing passes through LDS or between lanes:
@@ -22,9 +22,10 @@
 // entry a lane, one set ahead, and read out as scalars.  A skipped entry reads
 // a record of zeros, so the loads are unconditional; offsets are 64 bits.
 //
-// Work split: grid (unit, split), 4 waves taking steps round-robin over the
-// split's range; wave partials are merged through LDS and splits by a second
-// kernel, both in a fixed order.
+// Work split: a workgroup's 4 waves take the steps of its range round-robin;
+// their partials are merged through LDS and the parts of a unit that several
+// workgroups took by a second kernel, both in a fixed order (plan() says who
+// takes what).
 #include <algorithm>
 #include <cmath>
 
@@ -36,6 +37,8 @@ constexpr int D = ss::kHeadDim;
 constexpr int TOK = 32;  // tokens of a step
 constexpr int WAVES = 4;
 constexpr int CUS = 256;
+constexpr int kShares = 512;  // workgroups of SHARE, two a CU
+constexpr int kShareUnits = 40, kShareSteps = 512;  // from which they share (plan())
 constexpr int kMaxSplits = 256;
 constexpr int kMaxPartials = 4096;  // units * splits, where there is more than one split
 
@@ -90,10 +93,10 @@ __device__ __forceinline__ float rows_max(float x)
     return fmaxf(__uint_as_float(h[0]), __uint_as_float(h[1]));
 }
 
-// over all lanes, in every lane and in a fixed order
-template <class F>
-__device__ __forceinline__ float wave_fold(float x, const F &f)
+// maximum over the wave, in every lane
+__device__ __forceinline__ float wave_max(float x)
 {
+    auto f = [](float a, float b) { return fmaxf(a, b); };
     x = f(x, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), 0xB1, 0xF, 0xF, false)));   // lane ^ 1
     x = f(x, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), 0x4E, 0xF, 0xF, false)));   // lane ^ 2
     x = f(x, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), 0x141, 0xF, 0xF, false)));  // mirrored in 8 lanes
@@ -103,8 +106,13 @@ __device__ __forceinline__ float wave_fold(float x, const F &f)
     const auto h = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
     return f(__uint_as_float(h[0]), __uint_as_float(h[1]));
 }
-__device__ __forceinline__ float wave_max(float x) { return wave_fold(x, [](float a, float b) { return fmaxf(a, b); }); }
-__device__ __forceinline__ float wave_sum(float x) { return wave_fold(x, [](float a, float b) { return a + b; }); }
+
+// a value that is the same in every lane, in scalar registers
+__device__ __forceinline__ int64_t uniform(int64_t x)
+{
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)x), hi = __builtin_amdgcn_readfirstlane((uint32_t)(x >> 32));
+    return (int64_t)((uint64_t)hi << 32 | lo);
+}
 
 struct attn_args {
     const uint16_t *q;
@@ -119,11 +127,11 @@ struct attn_args {
     const int32_t *len;
     int Hq, Hkv, G, k;
     float scale_log2;
-    int steps_per_split;
+    int B, per;  // per: steps of a split (SPLIT)
     float *out, *ws;
 };
 
-// entries that unit u's sequence b can have: all k, or without a selection its blocks
+// entries that a unit of sequence b can have: all k, or without a selection its blocks
 __device__ __forceinline__ int entries_of(const attn_args &a, int b)
 {
     if (a.sel) return a.k;
@@ -131,8 +139,75 @@ __device__ __forceinline__ int entries_of(const attn_args &a, int b)
     return n < 0 ? 0 : min(n, a.k);
 }
 
-template <int BLK, int FMT>
-__global__ __launch_bounds__(WAVES * 64, 3) void attn_kv8_kernel(const attn_args a)
+// steps of a unit of sequence b, one at least
+template <int BLK>
+__device__ __forceinline__ uint32_t steps_of(const attn_args &a, int b)
+{
+    return max(1, (entries_of(a, b) * BLK + TOK - 1) / TOK);
+}
+
+// How the work is split.
+//   SPLIT: grid (unit, split), each split a->per steps of its unit.
+//   SHARE: the steps of all units stand in one line, unit after unit, and each
+//   of the workgroups takes the same share of it, whatever the units' lengths
+//   and however many there are (without a selection, where lengths differ).
+// Where a unit's steps fall to several workgroups a second kernel joins them.
+enum { SPLIT, SHARE };
+
+// The line, found the same way by every wave of both kernels.
+template <int BLK>
+struct line_t {
+    uint32_t total, share;
+    uint32_t mine, upto;  // sequence `lane`: its steps for one head, and with those of the sequences before
+
+    __device__ line_t(const attn_args &a, int lane)
+    {
+        mine = lane < a.B ? steps_of<BLK>(a, lane) : 0u;
+        upto = ss::wave_scan_sum(mine);
+        total = ss::lane_value(upto, 63);
+        for (int b = 64; b < a.B; b += 64)
+            total += ss::lane_value(ss::wave_scan_sum(b + lane < a.B ? steps_of<BLK>(a, b + lane) : 0u), 63);
+        total *= (uint32_t)a.Hkv;
+        share = ((total + kShares - 1) / kShares + WAVES - 1) / WAVES * WAVES;  // whole rounds of the waves
+    }
+    // the sequence of place x of the line, its steps for one head, and where it begins
+    __device__ void find(const attn_args &a, int lane, uint32_t x, int &b, uint32_t &steps, uint32_t &begin) const
+    {
+        uint32_t n = mine, sum = upto, before = 0;
+        for (int b0 = 0;;) {
+            const unsigned long long past = __ballot((before + sum) * a.Hkv > x);
+            if (past) {
+                const int l = __builtin_ctzll(past);
+                b = b0 + l;
+                steps = ss::lane_value(n, l);
+                begin = (before + ss::lane_value(sum, l) - steps) * a.Hkv;
+                return;
+            }
+            before += ss::lane_value(sum, 63);
+            b0 += 64;
+            n = b0 + lane < a.B ? steps_of<BLK>(a, b0 + lane) : 0u;
+            sum = ss::wave_scan_sum(n);
+        }
+    }
+    // where sequence b begins
+    __device__ uint32_t begin_of(const attn_args &a, int lane, int b) const
+    {
+        uint32_t before = 0;
+        for (int b0 = 0; b0 < b; b0 += 64) {
+            const int l = min(b - b0, 64) - 1;
+            before += ss::lane_value(b0 ? ss::wave_scan_sum(b0 + lane < a.B ? steps_of<BLK>(a, b0 + lane) : 0u) : upto, l);
+        }
+        return before * a.Hkv;
+    }
+};
+
+// Floats of a part of one head: maximum, sum, output.  SPLIT has room for a part
+// of each split, SHARE for two of each share (of its first unit, which may
+// have begun before, and of its last).
+constexpr int64_t kPartHead = D + 2;
+
+template <int BLK, int FMT, int MODE>
+__global__ __launch_bounds__(WAVES * 64, MODE == SPLIT ? 3 : 2) void attn_kv8_kernel(const attn_args a)
 {
     constexpr int REC = ss::kv8_record(BLK), OPEN = 2 * BLK * D * 2;
     constexpr int EPS = TOK / BLK;        // entries of a step
@@ -140,355 +215,439 @@ __global__ __launch_bounds__(WAVES * 64, 3) void attn_kv8_kernel(const attn_args
     __shared__ float sm_m[WAVES][16], sm_l[WAVES][16];
     __shared__ __align__(16) float sm_o[WAVES][16][D + 4];
 
-    const int u = blockIdx.x, split = blockIdx.y, splits = gridDim.y;
-    const int b = u / a.Hkv, g = u - b * a.Hkv;
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int L = lane >> 4, col = lane & 15;
-    const int n_entries = entries_of(a, b);
-    const int nsteps = (int)(((int64_t)n_entries * BLK + TOK - 1) / TOK);
-    const int s_begin = split * a.steps_per_split, s_end = min(s_begin + a.steps_per_split, nsteps);
-    const int open_rows = a.open ? max(a.len[b], 0) & (BLK - 1) : 0;
-    const bool tail = split == 0 && open_rows > 0;
-    float *part = a.ws + ((int64_t)u * splits + split) * a.G * (D + 2);
-    if (s_begin >= nsteps && !tail) {  // nothing here: the merge drops it by its maximum
-        if (splits > 1) {
-            if (threadIdx.x < a.G) part[threadIdx.x * (D + 2)] = -INFINITY;
-        } else {
-            for (int i = threadIdx.x; i < a.G * D; i += blockDim.x) a.out[((int64_t)b * a.Hq + g * a.G) * D + i] = 0.f;
-        }
-        return;
+    int b, u;                 // sequence and unit
+    int nsteps, first, last;  // the unit's steps, and the range taken here
+    uint32_t at_step = 0, end_step = 0, begin_step = 0;  // on the line
+    if (MODE == SHARE) {
+        const line_t<BLK> line(a, lane);
+        begin_step = blockIdx.x * line.share;
+        if (begin_step >= line.total) return;
+        uint32_t steps, begin;
+        line.find(a, lane, begin_step, b, steps, begin);
+        // the same in every lane, which the compiler does not see
+        b = __builtin_amdgcn_readfirstlane(b);
+        nsteps = __builtin_amdgcn_readfirstlane(steps);
+        begin = __builtin_amdgcn_readfirstlane(begin);
+        at_step = begin_step = __builtin_amdgcn_readfirstlane(begin_step);
+        end_step = __builtin_amdgcn_readfirstlane(min(begin_step + line.share, line.total));
+        const int g = (int)((at_step - begin) / (uint32_t)nsteps);
+        u = b * a.Hkv + g;
+        first = (int)(at_step - begin) - g * nsteps;
+        last = min(nsteps, first + (int)(end_step - at_step));
+    } else {
+        u = blockIdx.x;
+        b = u / a.Hkv;
+        nsteps = (int)steps_of<BLK>(a, b);
+        first = blockIdx.y * a.per;
+        last = min(first + a.per, nsteps);
+        if (first >= nsteps) return;
     }
 
-    // B operand of S^T: head `col`, channels 64*(m/2) + 16L + 8*(m%2) .. +7
-    frag_t qf[4];
-#pragma unroll
-    for (int m = 0; m < 4; ++m) {
-        const int h = col < a.G ? col : 0;
-        const u32x4_t w = *reinterpret_cast<const u32x4_t *>(a.q + ((int64_t)b * a.Hq + g * a.G + h) * D + 64 * (m >> 1) + 16 * L + 8 * (m & 1));
-        qf[m].u = col < a.G ? w : u32x4_t{0, 0, 0, 0};
-    }
+    for (;;) {
+        const int g = u - b * a.Hkv;
+        const int n_entries = entries_of(a, b);
+        const int s_begin = first, s_end = last;
+        const int open_rows = a.open ? __builtin_amdgcn_readfirstlane(max(a.len[b], 0) & (BLK - 1)) : 0;
+        const bool tail = first == 0 && open_rows > 0;
 
-    const gptr_t base = (gptr_t)(a.kv + a.region_off[u]);
-    int limit = a.slot_limit;
-    if (a.capacity) limit = min(limit, a.capacity[u]);
-    const int blocks = a.nblk ? a.nblk[b] : 0x7FFFFFFF;
-    // the page of entry i of the wave's steps from step `first` on, a lane each.
-    // What bounds an entry by the sequence's length is applied last, so that no
-    // load waits for the length.
-    auto resolve = [&](int first) {
-        const int st = first + (lane / EPS) * WAVES, e = st * EPS + lane % EPS;
-        int block = -1, page = -1;
-        if (e < a.k) block = a.sel ? a.sel[(int64_t)u * a.k + e] : e;
-        if (!a.tables) page = block;
-        else if (block >= 0 && block < a.max_blocks) page = a.tables[(int64_t)b * a.max_blocks + block];
-        return st < s_end && e < n_entries && block < blocks && page < limit ? page : -1;
-    };
-
-    float mrun = -INFINITY, lrun = 0.f;
-    f32x4_t o[8];
+        // B operand of S^T: head `col`, channels 64*(m/2) + 16L + 8*(m%2) .. +7
+        frag_t qf[4];
 #pragma unroll
-    for (int t = 0; t < 8; ++t) o[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-
-    // logits z (exp2 domain, -inf where masked) of the lane's tokens 4L + i of
-    // both subtiles, V scales and operand: one online softmax step
-    auto attend = [&](const float (&z)[8], float sv0, float sv1, auto &&vfrag) {
-        float cm = fmaxf(fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3])), fmaxf(fmaxf(z[4], z[5]), fmaxf(z[6], z[7])));
-        cm = rows_max(cm);
-        const float mnew = fmaxf(mrun, cm);
-        const float m0 = mnew == -INFINITY ? 0.f : mnew;  // nothing yet: every p is 0
-        if (__builtin_expect(__any(mnew != mrun), 0)) {
-            const float alpha = __builtin_amdgcn_exp2f(mrun - m0);
-#pragma unroll
-            for (int t = 0; t < 8; ++t) o[t] *= alpha;
-            lrun *= alpha;
-            mrun = mnew;
+        for (int m = 0; m < 4; ++m) {
+            const int h = col < a.G ? col : 0;
+            const u32x4_t w = *reinterpret_cast<const u32x4_t *>(a.q + ((int64_t)b * a.Hq + g * a.G + h) * D + 64 * (m >> 1) + 16 * L + 8 * (m & 1));
+            qf[m].u = col < a.G ? w : u32x4_t{0, 0, 0, 0};
         }
-        frag_t p1, p2, p3;
+
+        const gptr_t base = (gptr_t)(a.kv + uniform(a.region_off[u]));
+        int limit = a.slot_limit;
+        if (a.capacity) limit = min(limit, a.capacity[u]);
+        const int blocks = a.nblk ? a.nblk[b] : 0x7FFFFFFF;
+        // the page of entry i of the wave's steps from step `first` on, a lane each.
+        // What bounds an entry by the sequence's length is applied last, so that no
+        // load waits for the length.
+        auto resolve = [&](int first) {
+            const int st = first + (lane / EPS) * WAVES, e = st * EPS + lane % EPS;
+            int block = -1, page = -1;
+            if (e < a.k) block = a.sel ? a.sel[(int64_t)u * a.k + e] : e;
+            if (!a.tables) page = block;
+            else if (block >= 0 && block < a.max_blocks) page = a.tables[(int64_t)b * a.max_blocks + block];
+            return st < s_end && e < n_entries && block < blocks && page < limit ? page : -1;
+        };
+
+        float mrun = -INFINITY, lrun = 0.f;
+        f32x4_t o[8];
 #pragma unroll
-        for (int i = 0; i < 8; i += 2) {
-            float x[2];
+        for (int t = 0; t < 8; ++t) o[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+
+        // logits z (exp2 domain, -inf where masked) of the lane's tokens 4L + i of
+        // both subtiles, V scales and operand: one online softmax step
+        auto attend = [&](const float (&z)[8], float sv0, float sv1, auto &&vfrag) {
+            float cm = fmaxf(fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3])), fmaxf(fmaxf(z[4], z[5]), fmaxf(z[6], z[7])));
+            cm = rows_max(cm);
+            const float mnew = fmaxf(mrun, cm);
+            const float m0 = mnew == -INFINITY ? 0.f : mnew;  // nothing yet: every p is 0
+            if (__builtin_expect(__any(mnew != mrun), 0)) {
+                const float alpha = __builtin_amdgcn_exp2f(mrun - m0);
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const float p = __builtin_amdgcn_exp2f(z[i + h] - m0);
-                lrun += p;
-                x[h] = p * (i < 4 ? sv0 : sv1);
+                for (int t = 0; t < 8; ++t) o[t] *= alpha;
+                lrun *= alpha;
+                mrun = mnew;
             }
-            // three parts by truncation: each takes the upper half of what is left
-            auto upper = [&] { return __builtin_amdgcn_perm(__float_as_uint(x[1]), __float_as_uint(x[0]), 0x07060302); };
-            auto drop = [&](uint32_t w) {
-                x[0] -= __uint_as_float(w << 16);
-                x[1] -= __uint_as_float(w & 0xFFFF0000u);
-            };
-            p1.w[i >> 1] = upper();
-            drop(p1.w[i >> 1]);
-            p2.w[i >> 1] = upper();
-            drop(p2.w[i >> 1]);
-            p3.w[i >> 1] = upper();
-        }
-        // four accumulators in turn, so that none waits for its last product
+            frag_t p1, p2, p3;
 #pragma unroll
-        for (int t = 0; t < 8; t += 4) {
-            frag_t v[4];
+            for (int i = 0; i < 8; i += 2) {
+                float x[2];
 #pragma unroll
-            for (int h = 0; h < 4; ++h) v[h] = vfrag(t + h);
-#pragma unroll
-            for (int h = 0; h < 4; ++h) o[t + h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[h].v, p1.v, o[t + h], 0, 0, 0);
-#pragma unroll
-            for (int h = 0; h < 4; ++h) o[t + h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[h].v, p2.v, o[t + h], 0, 0, 0);
-#pragma unroll
-            for (int h = 0; h < 4; ++h) o[t + h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[h].v, p3.v, o[t + h], 0, 0, 0);
-            __builtin_amdgcn_sched_barrier(0);
-        }
-    };
-
-    gptr_t zeros = (gptr_t)zero_record;
-    asm("" : "+s"(zeros));  // its address is looked up once
-    struct step_t {
-        u32x4_t k[4], v[4];  // subtile 0, 1; channels 0..63, 64..127 (K), channel quads (V)
-        f32x2_t sc[2];       // scales of the lane's accumulator tokens
-        bool ok[2];
-    };
-    auto load_step = [&](const int (&page)[EPS], step_t &x) {
-        gptr_t rec[EPS];
-#pragma unroll
-        for (int e = 0; e < EPS; ++e) {
-            // both addresses first: a branch would hold the loads back
-            gptr_t r = base + (int64_t)page[e] * REC;
-            asm("" : "+s"(r));
-            rec[e] = page[e] >= 0 ? r : zeros;
-        }
-        auto get = [](gptr_t p) { return load_stream<u32x4_t>(p); };
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            if constexpr (BLK == 8) {
-                const bool kw = col >> 3, vw = L >> 1;  // which of the subtile's two records
-                const gptr_t kr = (kw ? rec[2 * s + 1] : rec[2 * s]) + L * 128 + (col & 7) * 16;
-                const gptr_t r = vw ? rec[2 * s + 1] : rec[2 * s];
-                const gptr_t vr = r + BLK * D + (L & 1) * 256 + col * 16;
-                x.k[2 * s] = get(kr);
-                x.k[2 * s + 1] = get(kr + 512);
-                x.v[2 * s] = get(vr);
-                x.v[2 * s + 1] = get(vr + 512);
-                x.sc[s] = load<f32x2_t>(r + 2 * BLK * D);
-                x.ok[s] = (vw ? page[2 * s + 1] : page[2 * s]) >= 0;
-            } else {
-                constexpr int PER = BLK / 16;  // subtiles of a record
-                const gptr_t r = rec[s / PER] + lane * 16;
-                x.k[2 * s] = get(r + (s % PER) * 2048);
-                x.k[2 * s + 1] = get(r + (s % PER) * 2048 + 1024);
-                x.v[2 * s] = get(r + BLK * D + (s % PER) * 2048);
-                x.v[2 * s + 1] = get(r + BLK * D + (s % PER) * 2048 + 1024);
-                x.sc[s] = load<f32x2_t>(rec[s / PER] + 2 * BLK * D);
-                x.ok[s] = page[s / PER] >= 0;
+                for (int h = 0; h < 2; ++h) {
+                    const float p = __builtin_amdgcn_exp2f(z[i + h] - m0);
+                    lrun += p;
+                    x[h] = p * (i < 4 ? sv0 : sv1);
+                }
+                // three parts by truncation: each takes the upper half of what is left
+                auto upper = [&] { return __builtin_amdgcn_perm(__float_as_uint(x[1]), __float_as_uint(x[0]), 0x07060302); };
+                auto drop = [&](uint32_t w) {
+                    x[0] -= __uint_as_float(w << 16);
+                    x[1] -= __uint_as_float(w & 0xFFFF0000u);
+                };
+                p1.w[i >> 1] = upper();
+                drop(p1.w[i >> 1]);
+                p2.w[i >> 1] = upper();
+                drop(p2.w[i >> 1]);
+                p3.w[i >> 1] = upper();
             }
-        }
-    };
-    auto compute_step = [&](const step_t &x) {
-        float z[8];
-        f32x4_t acc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+            // four accumulators in turn, so that none waits for its last product
 #pragma unroll
-        for (int m = 0; m < 4; ++m)
+            for (int t = 0; t < 8; t += 4) {
+                frag_t v[4];
+#pragma unroll
+                for (int h = 0; h < 4; ++h) v[h] = vfrag(t + h);
+#pragma unroll
+                for (int h = 0; h < 4; ++h) o[t + h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[h].v, p1.v, o[t + h], 0, 0, 0);
+#pragma unroll
+                for (int h = 0; h < 4; ++h) o[t + h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[h].v, p2.v, o[t + h], 0, 0, 0);
+#pragma unroll
+                for (int h = 0; h < 4; ++h) o[t + h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[h].v, p3.v, o[t + h], 0, 0, 0);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        };
+
+        gptr_t zeros = (gptr_t)zero_record;
+        asm("" : "+s"(zeros));  // its address is looked up once
+        struct step_t {
+            u32x4_t k[4], v[4];  // subtile 0, 1; channels 0..63, 64..127 (K), channel quads (V)
+            f32x2_t sc[2];       // scales of the lane's accumulator tokens
+            bool ok[2];
+        };
+        auto load_step = [&](const int (&page)[EPS], step_t &x) {
+            gptr_t rec[EPS];
+#pragma unroll
+            for (int e = 0; e < EPS; ++e) {
+                // both addresses first: a branch would hold the loads back
+                gptr_t r = base + (int64_t)page[e] * REC;
+                asm("" : "+s"(r));
+                rec[e] = page[e] >= 0 ? r : zeros;
+            }
+            auto get = [](gptr_t p) { return load_stream<u32x4_t>(p); };
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
-                frag_t f;
-                widen4<FMT>(x.k[2 * s + (m >> 1)][2 * (m & 1)], f.w[0], f.w[1]);
-                widen4<FMT>(x.k[2 * s + (m >> 1)][2 * (m & 1) + 1], f.w[2], f.w[3]);
-                acc[s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f.v, qf[m].v, acc[s], 0, 0, 0);
+                if constexpr (BLK == 8) {
+                    const bool kw = col >> 3, vw = L >> 1;  // which of the subtile's two records
+                    const gptr_t kr = (kw ? rec[2 * s + 1] : rec[2 * s]) + L * 128 + (col & 7) * 16;
+                    const gptr_t r = vw ? rec[2 * s + 1] : rec[2 * s];
+                    const gptr_t vr = r + BLK * D + (L & 1) * 256 + col * 16;
+                    x.k[2 * s] = get(kr);
+                    x.k[2 * s + 1] = get(kr + 512);
+                    x.v[2 * s] = get(vr);
+                    x.v[2 * s + 1] = get(vr + 512);
+                    x.sc[s] = load<f32x2_t>(r + 2 * BLK * D);
+                    x.ok[s] = (vw ? page[2 * s + 1] : page[2 * s]) >= 0;
+                } else {
+                    constexpr int PER = BLK / 16;  // subtiles of a record
+                    const gptr_t r = rec[s / PER] + lane * 16;
+                    x.k[2 * s] = get(r + (s % PER) * 2048);
+                    x.k[2 * s + 1] = get(r + (s % PER) * 2048 + 1024);
+                    x.v[2 * s] = get(r + BLK * D + (s % PER) * 2048);
+                    x.v[2 * s + 1] = get(r + BLK * D + (s % PER) * 2048 + 1024);
+                    x.sc[s] = load<f32x2_t>(rec[s / PER] + 2 * BLK * D);
+                    x.ok[s] = page[s / PER] >= 0;
+                }
             }
+        };
+        auto compute_step = [&](const step_t &x) {
+            float z[8];
+            f32x4_t acc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            const float sk = x.sc[s].x * a.scale_log2;
+            for (int m = 0; m < 4; ++m)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) z[4 * s + i] = x.ok[s] ? acc[s][i] * sk : -INFINITY;
-        }
-        attend(z, x.sc[0].y, x.sc[1].y, [&](int t) {
-            frag_t f;
-            widen4<FMT>(x.v[t >> 2][t & 3], f.w[0], f.w[1]);
-            widen4<FMT>(x.v[2 + (t >> 2)][t & 3], f.w[2], f.w[3]);
-            return f;
-        });
-    };
-
-    int st = s_begin + wave;
-    int pages = resolve(st), ahead = resolve(st + SET * WAVES);
-    int at = 0, later = st + 2 * SET * WAVES;  // the next step's place in the set; the set after `ahead`
-    auto load_next = [&](step_t &x) {
-        int page[EPS];
-#pragma unroll
-        for (int e = 0; e < EPS; ++e) page[e] = __builtin_amdgcn_readlane(pages, at * EPS + e);
-        load_step(page, x);
-        if (__builtin_expect(++at == SET, 0)) {
-            at = 0;
-            pages = ahead;
-            ahead = resolve(later);
-            later += SET * WAVES;
-        }
-    };
-
-    step_t bufA, bufB;
-    load_next(bufA);
-
-    if (tail && wave == WAVES - 1) {
-        // the open record: bf16 rows of K, channel-major V, tokens past the last not read
-        const uint8_t *ok = a.open + (int64_t)u * OPEN;
-        const uint16_t *ov = reinterpret_cast<const uint16_t *>(ok + BLK * D * 2);
-        float z[8];
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int m = 0; m < 4; ++m) {
-                frag_t f;
-                f.u = u32x4_t{0, 0, 0, 0};
-                if (16 * s + col < open_rows)
-                    f.u = *reinterpret_cast<const u32x4_t *>(ok + (16 * s + col) * (D * 2) + (64 * (m >> 1) + 16 * L + 8 * (m & 1)) * 2);
-                acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f.v, qf[m].v, acc, 0, 0, 0);
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) z[4 * s + i] = 16 * s + 4 * L + i < open_rows ? acc[i] * a.scale_log2 : -INFINITY;
-        }
-        attend(z, 1.f, 1.f, [&](int t) {
-            frag_t f;
+                for (int s = 0; s < 2; ++s) {
+                    frag_t f;
+                    widen4<FMT>(x.k[2 * s + (m >> 1)][2 * (m & 1)], f.w[0], f.w[1]);
+                    widen4<FMT>(x.k[2 * s + (m >> 1)][2 * (m & 1) + 1], f.w[2], f.w[3]);
+                    acc[s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f.v, qf[m].v, acc[s], 0, 0, 0);
+                }
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
-                const int tok = 16 * s + 4 * L, left = open_rows - tok;  // the lane's live tokens
-                u32x2_t w = {0, 0};
-                if (left > 0) w = *reinterpret_cast<const u32x2_t *>(ov + (8 * col + t) * BLK + tok);
-                f.w[2 * s] = left > 1 ? w.x : w.x & 0xFFFFu;
-                f.w[2 * s + 1] = left > 3 ? w.y : left > 2 ? w.y & 0xFFFFu : 0u;
+                const float sk = x.sc[s].x * a.scale_log2;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) z[4 * s + i] = x.ok[s] ? acc[s][i] * sk : -INFINITY;
             }
-            return f;
-        });
-    }
+            attend(z, x.sc[0].y, x.sc[1].y, [&](int t) {
+                frag_t f;
+                widen4<FMT>(x.v[t >> 2][t & 3], f.w[0], f.w[1]);
+                widen4<FMT>(x.v[2 + (t >> 2)][t & 3], f.w[2], f.w[3]);
+                return f;
+            });
+        };
 
-    for (; st < s_end; st += 2 * WAVES) {
-        load_next(bufB);
-        compute_step(bufA);
-        if (st + WAVES >= s_end) break;
+        int st = s_begin + wave;
+        int pages = resolve(st), ahead = resolve(st + SET * WAVES);
+        int at = 0, later = st + 2 * SET * WAVES;  // the next step's place in the set; the set after `ahead`
+        auto load_next = [&](step_t &x) {
+            int page[EPS];
+#pragma unroll
+            for (int e = 0; e < EPS; ++e) page[e] = __builtin_amdgcn_readlane(pages, at * EPS + e);
+            load_step(page, x);
+            if (__builtin_expect(++at == SET, 0)) {
+                at = 0;
+                pages = ahead;
+                ahead = resolve(later);
+                later += SET * WAVES;
+            }
+        };
+
+        step_t bufA, bufB;
         load_next(bufA);
-        compute_step(bufB);
-    }
-    lrun += __shfl_xor(lrun, 16);
-    lrun += __shfl_xor(lrun, 32);
 
-    // wave partials -> LDS; the lane holds channels 32L + 8i + t of head `col`
-    if (L == 0) {
-        sm_m[wave][col] = mrun;
-        sm_l[wave][col] = lrun;
-    }
-    if (col < a.G) {
+        if (tail && wave == WAVES - 1) {
+            // the open record: bf16 rows of K, channel-major V, tokens past the last not read
+            const uint8_t *ok = a.open + (int64_t)u * OPEN;
+            const uint16_t *ov = reinterpret_cast<const uint16_t *>(ok + BLK * D * 2);
+            float z[8];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            float *row = &sm_o[wave][col][32 * L + 8 * i];
-            *reinterpret_cast<f32x4_t *>(row) = f32x4_t{o[0][i], o[1][i], o[2][i], o[3][i]};
-            *reinterpret_cast<f32x4_t *>(row + 4) = f32x4_t{o[4][i], o[5][i], o[6][i], o[7][i]};
-        }
-    }
-    __syncthreads();
-    for (int idx = threadIdx.x; idx < a.G * D; idx += WAVES * 64) {
-        const int h = idx / D, ch = idx - h * D;
-        float M = sm_m[0][h];
+            for (int s = 0; s < 2; ++s) {
+                f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int w = 1; w < WAVES; ++w) M = fmaxf(M, sm_m[w][h]);
-        const float m0 = M == -INFINITY ? 0.f : M;
-        float lsum = 0.f, osum = 0.f;
+                for (int m = 0; m < 4; ++m) {
+                    frag_t f;
+                    f.u = u32x4_t{0, 0, 0, 0};
+                    if (16 * s + col < open_rows)
+                        f.u = *reinterpret_cast<const u32x4_t *>(ok + (16 * s + col) * (D * 2) + (64 * (m >> 1) + 16 * L + 8 * (m & 1)) * 2);
+                    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f.v, qf[m].v, acc, 0, 0, 0);
+                }
 #pragma unroll
-        for (int w = 0; w < WAVES; ++w) {
-            const float sc = __builtin_amdgcn_exp2f(sm_m[w][h] - m0);
-            lsum += sc * sm_l[w][h];
-            osum += sc * sm_o[w][h][ch];
-        }
-        if (splits == 1) {
-            a.out[((int64_t)b * a.Hq + g * a.G) * D + idx] = lsum == 0.f ? 0.f : osum / lsum;
-        } else {
-            float *pp = part + h * (D + 2);
-            if (ch == 0) {
-                // a split that saw only NaN logits is kept: its sums are NaN
-                pp[0] = M == -INFINITY && lsum != 0.f ? 0.f : M;
-                pp[1] = lsum;
+                for (int i = 0; i < 4; ++i) z[4 * s + i] = 16 * s + 4 * L + i < open_rows ? acc[i] * a.scale_log2 : -INFINITY;
             }
-            pp[2 + ch] = osum;
+            attend(z, 1.f, 1.f, [&](int t) {
+                frag_t f;
+#pragma unroll
+                for (int s = 0; s < 2; ++s) {
+                    const int tok = 16 * s + 4 * L, left = open_rows - tok;  // the lane's live tokens
+                    u32x2_t w = {0, 0};
+                    if (left > 0) w = *reinterpret_cast<const u32x2_t *>(ov + (8 * col + t) * BLK + tok);
+                    f.w[2 * s] = left > 1 ? w.x : w.x & 0xFFFFu;
+                    f.w[2 * s + 1] = left > 3 ? w.y : left > 2 ? w.y & 0xFFFFu : 0u;
+                }
+                return f;
+            });
         }
+
+        for (; st < s_end; st += 2 * WAVES) {
+            load_next(bufB);
+            compute_step(bufA);
+            if (st + WAVES >= s_end) break;
+            load_next(bufA);
+            compute_step(bufB);
+        }
+        lrun += __shfl_xor(lrun, 16);
+        lrun += __shfl_xor(lrun, 32);
+
+        // wave partials -> LDS; the lane holds channels 32L + 8i + t of head `col`
+        if (L == 0) {
+            sm_m[wave][col] = mrun;
+            sm_l[wave][col] = lrun;
+        }
+        if (col < a.G) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float *row = &sm_o[wave][col][32 * L + 8 * i];
+                *reinterpret_cast<f32x4_t *>(row) = f32x4_t{o[0][i], o[1][i], o[2][i], o[3][i]};
+                *reinterpret_cast<f32x4_t *>(row + 4) = f32x4_t{o[4][i], o[5][i], o[6][i], o[7][i]};
+            }
+        }
+        __syncthreads();
+        for (int idx = threadIdx.x; idx < a.G * D; idx += WAVES * 64) {
+            const int h = idx / D, ch = idx - h * D;
+            float M = sm_m[0][h];
+#pragma unroll
+            for (int w = 1; w < WAVES; ++w) M = fmaxf(M, sm_m[w][h]);
+            const float m0 = M == -INFINITY ? 0.f : M;
+            float lsum = 0.f, osum = 0.f;
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) {
+                const float sc = __builtin_amdgcn_exp2f(sm_m[w][h] - m0);
+                lsum += sc * sm_l[w][h];
+                osum += sc * sm_o[w][h][ch];
+            }
+            if (first == 0 && last == nsteps) {
+                a.out[((int64_t)b * a.Hq + g * a.G) * D + idx] = lsum == 0.f ? 0.f : osum / lsum;
+            } else {
+                const int64_t place = MODE == SHARE ? (int64_t)blockIdx.x * 2 + (at_step == begin_step ? 0 : 1)
+                                                    : (int64_t)u * gridDim.y + blockIdx.y;
+                float *pp = a.ws + (place * a.G + h) * kPartHead;
+                if (ch == 0) {
+                    // a part that saw only NaN logits is kept: its sums are NaN
+                    pp[0] = M == -INFINITY && lsum != 0.f ? 0.f : M;
+                    pp[1] = lsum;
+                }
+                pp[2 + ch] = osum;
+            }
+        }
+        if (MODE == SPLIT) return;
+        at_step += last - first;
+        if (at_step >= end_step) return;
+        ++u;
+        first = 0;
+        if (u - b * a.Hkv == a.Hkv) {
+            ++b;
+            nsteps = __builtin_amdgcn_readfirstlane((int)steps_of<BLK>(a, b));
+        }
+        last = min(nsteps, (int)(end_step - at_step));
+        __syncthreads();  // the partials in LDS have been read
     }
 }
 
-// Merges a unit's splits in their order, one workgroup per (unit, head), two
-// channels a lane.  Each of the W waves takes up to N splits, whose partials
-// it reads at once, beside all splits' maxima and sums (a split a lane): no
-// load waits for another.  A split without a token has the maximum -inf and
-// no partial.
-template <int W, int N>
-__global__ __launch_bounds__(W * 64) void combine_kv8_kernel(const float *__restrict__ ws, int Hq, int Hkv, int G,
-                                                             int splits, float *__restrict__ out)
+// Joins the parts of the units whose steps fell to several workgroups, in their
+// order: one workgroup per (unit, head), two channels a lane, 8 parts a wave
+// at a time, all read at once beside their maxima and sums.
+template <int BLK, int W, int MODE>
+__global__ __launch_bounds__(W * 64) void join_kv8_kernel(const attn_args a, int splits)
 {
-    constexpr int PER = (W * N + 63) / 64;  // splits of a lane
     typedef float f2_t __attribute__((ext_vector_type(2), aligned(4)));
+    __shared__ float s_m[W], s_l[W];
     __shared__ f32x2_t s_o[W][64];
     const int u = blockIdx.x, h = blockIdx.y, lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t stride = (int64_t)G * (D + 2);
-    const float *p = ws + (int64_t)u * splits * stride + h * (D + 2);
-    f2_t x[N];
-#pragma unroll
-    for (int i = 0; i < N; ++i) x[i] = *reinterpret_cast<const f2_t *>(p + min(wave * N + i, splits - 1) * stride + 2 + 2 * lane);
-    f2_t ml[PER];
-    float M = -INFINITY;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        ml[i] = f2_t{-INFINITY, 0.f};
-        if (i * 64 + lane < splits) ml[i] = *reinterpret_cast<const f2_t *>(p + (i * 64 + lane) * stride);
-        M = fmaxf(M, ml[i].x);
+    const int b = u / a.Hkv, g = u - b * a.Hkv;
+    const uint32_t steps = steps_of<BLK>(a, b);
+    uint32_t parts;
+    int64_t place0, place1;  // of the first part and the second; the others follow at the same distance
+    if (MODE == SHARE) {
+        const line_t<BLK> line(a, lane);
+        const uint32_t begin = line.begin_of(a, lane, b) + (uint32_t)g * steps, w0 = begin / line.share;
+        parts = (begin + steps - 1) / line.share - w0 + 1;
+        place0 = 2 * (int64_t)w0 + (begin != w0 * line.share ? 1 : 0);
+        place1 = 2 * (int64_t)w0 + 2;
+    } else {
+        parts = (steps + a.per - 1) / a.per;
+        place0 = (int64_t)u * splits;
+        place1 = place0 + 1;
     }
-    M = wave_max(M);
-    const float m0 = M == -INFINITY ? 0.f : M;
-    float w[PER], lsum = 0.f;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        w[i] = __builtin_amdgcn_exp2f(ml[i].x - m0);
-        lsum += ml[i].x == -INFINITY ? 0.f : w[i] * ml[i].y;
-    }
+    if (parts == 1) return;  // written by its one workgroup
+    auto part = [&](uint32_t i) {
+        return a.ws + ((i ? place1 + (int64_t)(i - 1) * (MODE == SHARE ? 2 : 1) : place0) * a.G + h) * kPartHead;
+    };
+    float M = -INFINITY, lsum = 0.f;
     f32x2_t osum = {0.f, 0.f};
+    for (uint32_t p0 = wave * 8; p0 < parts; p0 += W * 8) {
+        f2_t x[8];
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        const int s = wave * N + i;  // its weight: lane s % 64 of the s / 64-th
-        float own = w[0];
+        for (int i = 0; i < 8; ++i) x[i] = *reinterpret_cast<const f2_t *>(part(min(p0 + i, parts - 1)) + 2 + 2 * lane);
+        f2_t ml = {-INFINITY, 0.f};
+        if (lane < 8 && p0 + lane < parts) ml = *reinterpret_cast<const f2_t *>(part(p0 + lane));
+        const float mnew = fmaxf(M, wave_max(ml.x)), m0 = mnew == -INFINITY ? 0.f : mnew;
+        const float alpha = __builtin_amdgcn_exp2f(M - m0), w = __builtin_amdgcn_exp2f(ml.x - m0);
+        lsum *= alpha;
+        osum *= alpha;
+        M = mnew;
 #pragma unroll
-        for (int j = 1; j < PER; ++j) own = s / 64 == j ? w[j] : own;
-        const float sc = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(own), s % 64));
-        if (s < splits && sc != 0.f) {
-            osum.x += sc * x[i].x;
-            osum.y += sc * x[i].y;
+        for (int i = 0; i < 8; ++i) {
+            const float sc = __uint_as_float(ss::lane_value(__float_as_uint(w), i));
+            if (sc != 0.f) {  // parts past the last weigh nothing, whatever they hold
+                lsum += sc * __uint_as_float(ss::lane_value(__float_as_uint(ml.y), i));
+                osum.x += sc * x[i].x;
+                osum.y += sc * x[i].y;
+            }
         }
     }
-    if (wave) s_o[wave][lane] = osum;
-    if (W > 1) __syncthreads();
-    if (wave) return;
+    if (W > 1) {
+        s_o[wave][lane] = osum;
+        if (lane == 0) {
+            s_m[wave] = M;
+            s_l[wave] = lsum;
+        }
+        __syncthreads();
+        if (wave) return;
 #pragma unroll
-    for (int j = 1; j < W; ++j) {
-        osum.x += s_o[j][lane].x;
-        osum.y += s_o[j][lane].y;
+        for (int j = 1; j < W; ++j) M = fmaxf(M, s_m[j]);
+        const float m0 = M == -INFINITY ? 0.f : M;
+        lsum = 0.f;
+        osum = f32x2_t{0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < W; ++j) {
+            const float sc = __builtin_amdgcn_exp2f(s_m[j] - m0);
+            lsum += sc * s_l[j];
+            osum.x += sc * s_o[j][lane].x;
+            osum.y += sc * s_o[j][lane].y;
+        }
     }
-    lsum = wave_sum(lsum);
     f2_t y = {0.f, 0.f};
     if (lsum != 0.f) y = f2_t{osum.x / lsum, osum.y / lsum};
-    const int b = u / Hkv, g = u - b * Hkv;
-    *reinterpret_cast<f2_t *>(out + ((int64_t)b * Hq + g * G + h) * D + 2 * lane) = y;
+    *reinterpret_cast<f2_t *>(a.out + ((int64_t)b * a.Hq + g * a.G + h) * D + 2 * lane) = y;
 }
 
 struct split_plan {
-    int splits, steps_per_split;
+    int mode, splits, per;
 };
 
-// Splits per unit: three workgroups a CU, 8 steps or more each.
-split_plan plan(int64_t units, int k, int blk, int most)
+// SHARE where a call attends to all blocks of sequences whose lengths only the
+// GPU knows, and there are enough units to cover all CUs with long pieces (us,
+// SPLIT and SHARE, lengths from an eighth of the longest on): 44 units of up
+// to 512 steps 31.0, 28.9; 128 of 512 77.5, 70.7; 44 of 2048 103, 76; 64 of
+// 2048 129, 120; a real batch of 128 of 2048 220, 180.  Few units are split
+// evenly anyway (32 of 512 21.7, 23.2; 12 of 2048 35.3, 37.7), and where a
+// share has several units their beginnings add up (512 of 128 68.6, 73.2; 128
+// of 128 23.9, 26.2).
+//
+// SPLIT takes the splits that cost least by a model of the time (us; fitted to
+// 1875 shapes of 1 to 1024 units, 1 to 4096 steps, G 1 to 16, each block size
+// and format: its choices lose 0.6% against the best on average, three
+// workgroups a CU lose 5%, up to 50%):
+//   - the chip's bandwidth: kStepHbm a step;
+//   - the fullest CU: a workgroup's waves take a step each per round, of
+//     kRound1 alone on the CU, kRound2 beside another, kRound3 for each of more;
+//     kGroup a workgroup besides;
+//   - the join, a second launch.
+split_plan plan(int64_t units, int k, int blk, int G, bool selected, size_t room)
 {
     const int steps = (int)(((int64_t)k * blk + TOK - 1) / TOK);
-    int64_t n = std::min<int64_t>((3 * CUS + units - 1) / units, std::max(1, steps / 8));
-    n = std::min<int64_t>(n, std::min<int64_t>(most, kMaxPartials / std::max<int64_t>(units, 1)));
-    n = std::max<int64_t>(n, 1);
-    const int per = (int)((steps + n - 1) / n);
-    return {(steps + per - 1) / per, per};
+    const int64_t all = units * steps;
+    const size_t part = G * kPartHead * sizeof(float);
+    if (!selected && units >= kShareUnits && steps >= kShareSteps && all <= 0x7FFFFFFF && room >= 2 * kShares * part)
+        return {SHARE, kShares, 0};
+    constexpr float kStepHbm = 0.00096f, kRound1 = 0.73f, kRound2 = 1.6f, kRound3 = 0.84f, kGroup = 0.2f, kBoth = 0.088f;
+    constexpr float kJoin = 2.61f, kJoinSplit = 0.012f, kJoinGroup = 0.00045f, kJoinHead = 0.00012f;
+    const int64_t most = std::min<int64_t>(std::min<int64_t>(kMaxSplits, room / part / units), kMaxPartials / units);
+    int best = 1;
+    float least = 0.f;
+    for (int n = 1; n == 1 || (n <= most && n <= steps); ++n) {
+        const int per = (steps + n - 1) / n, splits = (steps + per - 1) / per;
+        if (n > 1 && splits < n) continue;  // the same as with fewer
+        const float groups = (float)units * splits, fullest = std::ceil(groups / CUS), rounds = (float)((per + WAVES - 1) / WAVES);
+        const float hbm = all * kStepHbm;
+        const float cu = rounds * (fullest == 1.f ? kRound1 : fullest == 2.f ? kRound2 : kRound3 * fullest) + kGroup * fullest;
+        float cost = std::max(hbm, cu) + kBoth * std::min(hbm, cu);
+        if (splits > 1) cost += kJoin + kJoinSplit * splits + (kJoinGroup + kJoinHead * G) * groups;
+        if (n == 1 || cost < least) {
+            best = n;
+            least = cost;
+        }
+    }
+    const int per = (steps + best - 1) / best;
+    return {SPLIT, (steps + per - 1) / per, per};
 }
 
 bool has_plan(int B, int Hq, int Hkv, int d, int blk, int k)
@@ -496,12 +655,24 @@ bool has_plan(int B, int Hq, int Hkv, int d, int blk, int k)
     return B > 0 && Hkv > 0 && Hq > 0 && Hq % Hkv == 0 && d == D && ss::supported_blk(blk) && k > 0;
 }
 
-size_t split_bytes(int B, int Hq) { return (size_t)B * Hq * (D + 2) * sizeof(float); }
+// bytes of a plan's parts
+size_t plan_bytes(const split_plan &p, int64_t units, int G)
+{
+    const size_t part = G * kPartHead * sizeof(float);
+    return p.mode == SHARE ? 2 * kShares * part : p.splits > 1 ? units * p.splits * part : 0;
+}
 
-template <int FMT>
+template <int BLK>
+auto join_of(int mode, int waves)
+{
+    if (mode == SHARE) return join_kv8_kernel<BLK, 8, SHARE>;
+    return waves == 1 ? join_kv8_kernel<BLK, 1, SPLIT> : waves == 4 ? join_kv8_kernel<BLK, 4, SPLIT> : join_kv8_kernel<BLK, 8, SPLIT>;
+}
+
+template <int FMT, int MODE>
 auto attn_of(int blk)
 {
-    return blk == 8 ? attn_kv8_kernel<8, FMT> : blk == 16 ? attn_kv8_kernel<16, FMT> : attn_kv8_kernel<32, FMT>;
+    return blk == 8 ? attn_kv8_kernel<8, FMT, MODE> : blk == 16 ? attn_kv8_kernel<16, FMT, MODE> : attn_kv8_kernel<32, FMT, MODE>;
 }
 
 }  // namespace
@@ -509,8 +680,11 @@ auto attn_of(int blk)
 extern "C" size_t ss_sparse_attention_kv8_workspace(int B, int Hq, int Hkv, int d, int blk, int k)
 {
     if (!has_plan(B, Hq, Hkv, d, blk, k)) return 0;
-    const int splits = plan((int64_t)B * Hkv, k, blk, kMaxSplits).splits;
-    return splits > 1 ? splits * split_bytes(B, Hq) : 0;
+    // what a call takes depends on whether it selects: room for either
+    const int64_t units = (int64_t)B * Hkv;
+    const int G = Hq / Hkv;
+    const size_t any = ~(size_t)0 >> 1;
+    return std::max(plan_bytes(plan(units, k, blk, G, false, any), units, G), plan_bytes(plan(units, k, blk, G, true, any), units, G));
 }
 
 extern "C" ss_status ss_sparse_attention_kv8(const void *q, const void *kv_base, const int64_t *region_off,
@@ -538,26 +712,21 @@ extern "C" ss_status ss_sparse_attention_kv8(const void *q, const void *kv_base,
                  "ss_sparse_attention_kv8: buffers must be 16-byte aligned");
     const int64_t units = (int64_t)B * Hkv;
     SS_CHECK_SUPPORTED(units <= 0x7FFFFFFF / (WAVES * 64), "ss_sparse_attention_kv8: %lld units pass the launch", (long long)units);
-    const size_t room = workspace ? ws_bytes / split_bytes(B, Hq) : 0;
-    const split_plan sp = plan(units, k, blk, (int)std::max<size_t>(1, std::min(room, (size_t)kMaxSplits)));
     const int G = Hq / Hkv;
+    const split_plan sp = plan(units, k, blk, G, sel != nullptr, workspace ? ws_bytes : 0);
     const attn_args a = {static_cast<const uint16_t *>(q), static_cast<const uint8_t *>(kv_base), region_off, sel, tables,
                          max_blocks, capacity, slot_limit, nblk, static_cast<const uint8_t *>(open_blocks), len, Hq, Hkv, G,
-                         k, scale * 1.4426950408889634f, sp.steps_per_split, out, static_cast<float *>(workspace)};
+                         k, scale * 1.4426950408889634f, B, sp.per, out, static_cast<float *>(workspace)};
     hipStream_t s = ss::as_stream(stream);
-    ss::launch(fmt == SS_KV8_E4M3 ? attn_of<SS_KV8_E4M3>(blk) : attn_of<SS_KV8_INT8>(blk), dim3((unsigned)units, sp.splits),
-               dim3(WAVES * 64), s, a);
+    const bool e4m3 = fmt == SS_KV8_E4M3;
+    auto *kernel = e4m3 ? attn_of<SS_KV8_E4M3, SPLIT>(blk) : attn_of<SS_KV8_INT8, SPLIT>(blk);
+    if (sp.mode == SHARE) kernel = e4m3 ? attn_of<SS_KV8_E4M3, SHARE>(blk) : attn_of<SS_KV8_INT8, SHARE>(blk);
+    const dim3 grid = sp.mode == SHARE ? dim3(kShares) : dim3((unsigned)units, sp.splits);
+    ss::launch(kernel, grid, dim3(WAVES * 64), s, a);
     ss_status st = ss::check_launch("ss_sparse_attention_kv8");
     if (st != SS_OK || sp.splits == 1) return st;
-    // reads as many partials as there may be splits
-    auto *combine = combine_kv8_kernel<16, 16>;
-    int waves = 16;
-    if (sp.splits <= 4) combine = combine_kv8_kernel<1, 4>, waves = 1;
-    else if (sp.splits <= 8) combine = combine_kv8_kernel<1, 8>, waves = 1;
-    else if (sp.splits <= 16) combine = combine_kv8_kernel<2, 8>, waves = 2;
-    else if (sp.splits <= 32) combine = combine_kv8_kernel<4, 8>, waves = 4;
-    else if (sp.splits <= 64) combine = combine_kv8_kernel<8, 8>, waves = 8;
-    else if (sp.splits <= 128) combine = combine_kv8_kernel<16, 8>, waves = 16;
-    combine<<<dim3((unsigned)units, G), dim3(waves * 64), 0, s>>>(a.ws, Hq, Hkv, G, sp.splits, out);
-    return ss::check_launch("ss_sparse_attention_kv8(merge)");
+    const int waves = sp.mode == SHARE || sp.splits > 32 ? 8 : sp.splits > 8 ? 4 : 1;  // 8 parts each
+    auto *join = blk == 8 ? join_of<8>(sp.mode, waves) : blk == 16 ? join_of<16>(sp.mode, waves) : join_of<32>(sp.mode, waves);
+    join<<<dim3((unsigned)units, G), dim3(waves * 64), 0, s>>>(a, sp.splits);
+    return ss::check_launch("ss_sparse_attention_kv8(join)");
 }

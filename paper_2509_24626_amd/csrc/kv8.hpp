@@ -38,6 +38,20 @@ __device__ __forceinline__ int find_item(const int32_t *__restrict__ begin, int 
     return lo;
 }
 
+// inclusive sum over the wave's lanes
+__device__ __forceinline__ uint32_t wave_scan_sum(uint32_t x)
+{
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x111, 0xF, 0xF, false);  // row_shr 1, 2, 4, 8
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x112, 0xF, 0xF, false);
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x114, 0xF, 0xF, false);
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x118, 0xF, 0xF, false);
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x142, 0xA, 0xF, false);  // lane 15 of rows 0, 2 to rows 1, 3
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x143, 0xC, 0xF, false);  // lane 31 to rows 2, 3
+    return x;
+}
+
+__device__ __forceinline__ uint32_t lane_value(uint32_t x, int lane) { return (uint32_t)__builtin_amdgcn_readlane((int)x, lane); }
+
 // the other value of a lane pair (lane ^ 1)
 __device__ __forceinline__ uint32_t pair_swap(uint32_t x)
 {

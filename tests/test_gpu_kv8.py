@@ -780,3 +780,24 @@ def test_serving_step_in_a_graph(ss):
         o.check()
         if i == 4:
             s.finish(np.eye(1, B, 2)[0])
+
+
+# ------------------------------------- equal shares of all sequences' steps
+@pytest.mark.parametrize("blk, fmt, B, hkv, G, longest", [
+    (8, 0, 14, 3, 4, 2100), (16, 1, 150, 2, 1, 300), (32, 0, 70, 1, 7, 200), (16, 0, 20, 2, 16, 400), (32, 1, 40, 1, 2, 20)])
+def test_attention_of_long_tables_shared_out(ss, blk, fmt, B, hkv, G, longest):
+    """Tables long enough that the workgroups share the steps of all
+    sequences: lengths from nothing to `longest` blocks, so that shares begin
+    and end inside units, span several, and units lie in one share or many."""
+    rng = np.random.default_rng(71 + blk + B)
+    length = (longest * blk * rng.random(B) ** 3).astype(int)
+    length[rng.integers(B)] = longest * blk
+    length[0] = 0
+    k = max(longest, 512 * 32 // blk)
+    s = Stored(rng, blk, fmt, length, hkv, G).to_device()
+    first = attend(ss, s, None, k, with_open=True)
+    worst = s.check(first, lambda b, g: range(s.nblk[b]), True)
+    small = attend(ss, s, None, k, with_open=True, room=G * 130 * 4 * B * hkv)  # room for no share
+    s.check(small, lambda b, g: range(s.nblk[b]), True)
+    print(f"[gpu] max abs error {worst:.2e}")
+    assert torch.equal(first, attend(ss, s, None, k, with_open=True))

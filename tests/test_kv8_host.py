@@ -127,42 +127,50 @@ def test_record_and_workspace_sizes():
         assert ss.ss_kv8_record_bytes(blk, 128) == ref.record_bytes(blk)
     assert ss.ss_kv8_record_bytes(64, 128) == ss.ss_kv8_record_bytes(16, 64) == 0
     w = ss.ss_sparse_attention_kv8_workspace(1, 32, 8, 128, 16, 4096)
-    assert w > 0 and w % (32 * 130 * 4) == 0
+    assert w > 0 and w % (4 * 130 * 4) == 0
     assert ss.ss_sparse_attention_kv8_workspace(2, 8, 2, 128, 16, 2) == 0
     assert ss.ss_sparse_attention_kv8_workspace(1, 30, 8, 128, 16, 64) == 0
 
 
 LAUNCHES = r"""
 P, got = 0x1000, []
-for B, Hq, Hkv, blk, k in json.loads(sys.argv[2]):
+for B, Hq, Hkv, blk, k, all_blocks in json.loads(sys.argv[2]):
     one = B * Hq * 130 * 4
     query = ss.ss_sparse_attention_kv8_workspace(B, Hq, Hkv, 128, blk, k)
     made = []
     for size in (0, one - 1, one, 2 * one, query // 2, query, 4 * query):
-        ss.ss_sparse_attention_kv8(P, P, P, P, None, 0, None, 64, None, None, None, 0, B, Hq, Hkv, 128, blk, k, 0.1, P,
-                                   P if size else None, size, stream=0)
+        ss.ss_sparse_attention_kv8(P, P, P, None if all_blocks else P, P, k, None, 64, P, None, None, 0, B, Hq, Hkv, 128, blk,
+                                   k, 0.1, P, P if size else None, size, stream=0)
         made.append([size, launches()])
-    got.append({"one": one, "query": query, "made": made})
+    got.append({"query": query, "made": made})
 print(json.dumps(got))
 """
 
 
 def test_attention_takes_every_workspace_size():
-    """Whatever the workspace, the partials of the launch that it gets fit it."""
+    """Whatever the workspace, the parts of the launch that it gets fit it: a
+    part of each split of each unit, or two of each of 512 shares."""
     import tempfile
     stand_in = hip_stand_in.build(tempfile.mkdtemp()) or pytest.skip("no C compiler")
-    shapes = [(B, hkv * G, hkv, blk, k) for B in (1, 3, 64, 700, 5000) for hkv, G in ((1, 1), (8, 4), (4, 7), (2, 16))
+    shapes = [(B, hkv * G, hkv, blk, k, every) for B in (1, 3, 64, 700, 5000)
+              for hkv, G in ((1, 1), (8, 4), (4, 7), (2, 16)) for every in (False, True)
               for blk, k in ((8, 1), (16, 128), (32, 511), (8, 16384), (32, 65536))]
-    for (B, Hq, Hkv, blk, k), c in zip(shapes, json.loads(hip_stand_in.run(stand_in, LAUNCHES, json.dumps(shapes)))):
+    shared = 0
+    for (B, Hq, Hkv, blk, k, every), c in zip(shapes, json.loads(hip_stand_in.run(stand_in, LAUNCHES, json.dumps(shapes)))):
+        steps, part = -(-k * blk // 32), Hq // Hkv * 130 * 4
         for size, made in c["made"]:
             grid = made[0]
+            if len(made) == 2 and grid[1] == 1:
+                assert every and grid[0] == 512 and 2 * 512 * part <= size and B * Hkv >= 40 and steps >= 512
+                shared += 1
+                continue
             assert grid[0] == B * Hkv and len(made) == (1 if grid[1] == 1 else 2)
             if grid[1] > 1:
-                assert grid[1] * c["one"] <= size
-                assert grid[0] * grid[1] <= 4096
-        full = next(m for s, m in c["made"] if s == c["query"])  # the query's size is all that is ever used
-        assert c["made"][-1][1] == full
-        assert c["query"] == (full[0][1] * c["one"] if full[0][1] > 1 else 0)
+                assert grid[0] * grid[1] * part <= size
+                assert grid[0] * grid[1] <= 4096 and grid[1] <= steps
+        # the query's size is all that is ever used
+        assert c["made"][-1][1] == next(m for s, m in c["made"] if s == c["query"])
+    assert shared > 10
 
 
 def test_layout_is_a_permutation():
