@@ -283,6 +283,8 @@ ss_status ss_dev_cache_total_misses(const ss_dev_cache *cache, int64_t *total);
  *   pool_base: device address of the pool (mapped host memory or HBM)
  *   pool_off, cache_off: device int64 [B*Hkv] byte offsets
  *   nblk: device int32 [B]; capacity: device int32 [B*Hkv]
+ *   record_bytes: that of a bf16 record (2*blk*d*2) or of a record in 8 bits
+ *       (ss_kv8_record_bytes)
  * Rows with b, g, block or slot out of range are skipped. */
 ss_status ss_gather_blocks(const int32_t *miss, int64_t n_miss, const void *pool_base, const int64_t *pool_off,
                            void *cache_base, const int64_t *cache_off, const int32_t *nblk,

@@ -2,7 +2,8 @@
 // kernel copies every missed block record from the pinned, device-mapped
 // DRAM pool into its HBM cache slot, instead of one memcpy per block.
 //
-// Each workgroup copies whole records (4, 8 or 16 KiB).  Every thread issues
+// Each workgroup copies whole records (4, 8 or 16 KiB, or half of that and a
+// trailer in 8 bits).  Every thread issues
 // all of its 16-byte loads for RPI records before the first store, so each
 // wave keeps RPI*CH KiB of host-link reads in flight; workgroups stride over
 // the miss list.  The grid is small on purpose: a launch-shape sweep on
@@ -23,13 +24,13 @@
 // and no cross-engine synchronisation, sits between resolve and attention.
 #include <climits>
 
-#include "internal.hpp"
+#include "kv8.hpp"
 
 namespace {
 
 typedef unsigned int u32x4_t __attribute__((ext_vector_type(4)));
 
-template <int CH, int RPI>  // 16-byte chunks per thread per record; records per iteration
+template <int N16, int RPI>  // 16-byte chunks per record; records per iteration
 __global__ __launch_bounds__(256) void gather_kernel(const int4 *__restrict__ miss, int64_t n_miss,
                                                      const uint8_t *__restrict__ pool,
                                                      const int64_t *__restrict__ pool_off,
@@ -40,7 +41,8 @@ __global__ __launch_bounds__(256) void gather_kernel(const int4 *__restrict__ mi
                                                      const int32_t *__restrict__ copy_src,
                                                      int32_t *__restrict__ copy_dst, int64_t copy_n)
 {
-    constexpr int64_t REC = 4096LL * CH;
+    constexpr int64_t REC = 16LL * N16;
+    constexpr int CH = (N16 + 255) / 256;  // of a thread; the last of an 8-bit record has its trailer only
     const int t = threadIdx.x;
     for (int64_t i = (int64_t)blockIdx.x * 256 + t; i < copy_n; i += (int64_t)gridDim.x * 256) copy_dst[i] = copy_src[i];
     for (int64_t m0 = (int64_t)blockIdx.x * RPI; m0 < n_miss; m0 += (int64_t)gridDim.x * RPI) {
@@ -70,13 +72,15 @@ __global__ __launch_bounds__(256) void gather_kernel(const int4 *__restrict__ mi
         for (int r = 0; r < RPI; ++r)
             if (ok[r]) {
 #pragma unroll
-                for (int c = 0; c < CH; ++c) v[r][c] = __builtin_nontemporal_load(src[r] + c * 256 + t);
+                for (int c = 0; c < CH; ++c)
+                    if ((c + 1) * 256 <= N16 || c * 256 + t < N16) v[r][c] = __builtin_nontemporal_load(src[r] + c * 256 + t);
             }
 #pragma unroll
         for (int r = 0; r < RPI; ++r)
             if (ok[r]) {
 #pragma unroll
-                for (int c = 0; c < CH; ++c) __builtin_nontemporal_store(v[r][c], &dst[r][c * 256 + t]);
+                for (int c = 0; c < CH; ++c)
+                    if ((c + 1) * 256 <= N16 || c * 256 + t < N16) __builtin_nontemporal_store(v[r][c], &dst[r][c * 256 + t]);
             }
     }
 }
@@ -183,7 +187,7 @@ __global__ __launch_bounds__(256) void gather_units_kernel(const int4 *__restric
     }
 }
 
-template <int CH>
+template <int N16>
 void launch_variant(const int4 *miss, int64_t n_miss, const uint8_t *pool, const int64_t *pool_off, uint8_t *cache,
             const int64_t *cache_off, const int32_t *nblk, const int32_t *cap, int B, int Hkv,
             const int32_t *copy_src, int32_t *copy_dst, int64_t copy_n, hipStream_t s)
@@ -192,10 +196,10 @@ void launch_variant(const int4 *miss, int64_t n_miss, const uint8_t *pool, const
     int64_t blocks = (n_miss + RPI - 1) / RPI;
     // about 512 KiB of records in flight per launch: 32 workgroups of two 8 KiB
     // records, 64 of 4 KiB, 16 of 16 KiB
-    const int64_t max_blocks = 32 * 2 / CH;
+    const int64_t max_blocks = (512 << 10) / (RPI * 16 * N16);
     if (blocks > max_blocks) blocks = max_blocks;
     if (blocks < 1) blocks = 1;
-    ss::launch(gather_kernel<CH, RPI>, dim3((unsigned)blocks), dim3(256), s, miss, n_miss, pool, pool_off, cache,
+    ss::launch(gather_kernel<N16, RPI>, dim3((unsigned)blocks), dim3(256), s, miss, n_miss, pool, pool_off, cache,
                cache_off, nblk, cap, B, Hkv, copy_src, copy_dst, copy_n);
 }
 
@@ -244,11 +248,15 @@ ss_status launch_gather(const int32_t *miss, int64_t n_miss, const void *pool_ba
     const int4 *m = reinterpret_cast<const int4 *>(miss);
     const uint8_t *p = static_cast<const uint8_t *>(pool_base);
     uint8_t *c = static_cast<uint8_t *>(cache_base);
+    auto *launch = launch_variant<1024>;
     switch (record_bytes) {
-    case 4096: launch_variant<1>(m, n_miss, p, pool_off, c, cache_off, nblk, capacity, B, Hkv, copy_src, copy_dst, copy_n, s); break;
-    case 8192: launch_variant<2>(m, n_miss, p, pool_off, c, cache_off, nblk, capacity, B, Hkv, copy_src, copy_dst, copy_n, s); break;
-    default: launch_variant<4>(m, n_miss, p, pool_off, c, cache_off, nblk, capacity, B, Hkv, copy_src, copy_dst, copy_n, s); break;
+    case 4096: launch = launch_variant<256>; break;
+    case 8192: launch = launch_variant<512>; break;
+    case kv8_record(8): launch = launch_variant<kv8_record(8) / 16>; break;
+    case kv8_record(16): launch = launch_variant<kv8_record(16) / 16>; break;
+    case kv8_record(32): launch = launch_variant<kv8_record(32) / 16>; break;
     }
+    launch(m, n_miss, p, pool_off, c, cache_off, nblk, capacity, B, Hkv, copy_src, copy_dst, copy_n, s);
     return check_launch("ss_gather_blocks");
 }
 
@@ -261,8 +269,10 @@ extern "C" ss_status ss_gather_blocks(const int32_t *miss, int64_t n_miss, const
 {
     SS_CHECK_ARG(n_miss >= 0 && B >= 0 && Hkv > 0, "ss_gather_blocks: bad shape n_miss=%lld B=%d Hkv=%d",
                  (long long)n_miss, B, Hkv);
-    SS_CHECK_SUPPORTED(record_bytes == 4096 || record_bytes == 8192 || record_bytes == 16384,
-                       "ss_gather_blocks: record_bytes=%zu (blk 8/16/32 at d=128)", record_bytes);
+    bool known = false;
+    for (int blk = 8; blk <= 32; blk *= 2)
+        known = known || record_bytes == (size_t)4 * blk * ss::kHeadDim || record_bytes == (size_t)ss::kv8_record(blk);
+    SS_CHECK_SUPPORTED(known, "ss_gather_blocks: record_bytes=%zu (blk 8/16/32 at d=128, bf16 or 8 bits)", record_bytes);
     if (n_miss == 0) return SS_OK;
     SS_CHECK_ARG(miss && pool_base && pool_off && cache_base && cache_off && nblk && capacity,
                  "ss_gather_blocks: null pointer");

@@ -801,3 +801,101 @@ def test_attention_of_long_tables_shared_out(ss, blk, fmt, B, hkv, G, longest):
     s.check(small, lambda b, g: range(s.nblk[b]), True)
     print(f"[gpu] max abs error {worst:.2e}")
     assert torch.equal(first, attend(ss, s, None, k, with_open=True))
+
+
+# ------------------------------------------------- records in host memory
+@pytest.mark.parametrize("blk", [8, 16, 32])
+def test_gather_of_8_bit_records(ss, blk):
+    """Missed records from mapped host memory into cache slots, byte for byte;
+    rows out of range are skipped and other slots keep their bytes."""
+    import ctypes
+    rng = np.random.default_rng(81)
+    rec, B, hkv, blocks, slots = ref.record_bytes(blk), 3, 2, 70, 9
+    size = B * hkv * blocks * rec
+    addr, mapped = ss.ss_host_alloc_mapped(size)
+    pool = np.ctypeslib.as_array((ctypes.c_uint8 * size).from_address(addr)).reshape(B * hkv, blocks, rec)
+    pool[:] = rng.integers(0, 256, pool.shape)
+    cache = empty(B * hkv, slots, rec, fill=0x11, dtype=torch.uint8)
+    want = np.full(cache.shape, 0x11, np.uint8)
+    miss = [(b, g, int(rng.integers(blocks)), int(s)) for b in range(B) for g in range(hkv)
+            for s in rng.permutation(slots)[:int(rng.integers(1, slots))]]
+    for b, g, j, s in miss:
+        want[b * hkv + g, s] = pool[b * hkv + g, j]
+    bad = [(B, 0, 0, 0), (0, hkv, 0, 0), (0, 0, blocks, 0), (0, 0, 0, slots), (-1, 0, 0, 0), (0, 0, -1, 0)]
+    rows = dev(miss[:5] + bad + miss[5:])
+    off = lambda n: dev(np.arange(B * hkv) * n * rec, np.int64)  # noqa: E731
+    ss.ss_gather_blocks(rows, len(rows), mapped, off(blocks), cache, off(slots), dev([blocks] * B),
+                        dev([slots] * (B * hkv)), B, hkv, rec)
+    got = host(cache)
+    ss.ss_host_free(addr)
+    assert np.array_equal(got, want)
+
+
+@pytest.mark.parametrize("blk, fmt", [(16, 0), (8, 1)])
+def test_steps_over_a_hierarchical_cache_in_8_bits(ss, blk, fmt):
+    """Prompts and single tokens written in 8 bits straight to the DRAM pool;
+    each step scores, selects, resolves the slot tables, gathers the missing
+    records and attends over the HBM cache's slots."""
+    import ctypes
+    rng = np.random.default_rng(82)
+    rec, B, hkv, G, room, k, slots = ref.record_bytes(blk), 3, 2, 4, 40, 6, 9
+    size = B * hkv * room * rec
+    addr, mapped = ss.ss_host_alloc_mapped(size)
+    pool = np.ctypeslib.as_array((ctypes.c_uint8 * size).from_address(addr))
+    pool[:] = 0
+    units = B * hkv
+    pool_off, cache_off = (dev(np.arange(units) * n * rec, np.int64) for n in (room, slots))
+    open_blocks = torch.zeros(B, hkv, 2 * blk * D, dtype=torch.bfloat16, device="cuda")
+    meta = torch.zeros(B, hkv, room, 2, D, dtype=torch.bfloat16, device="cuda")
+    cache = torch.zeros(units, slots, rec, dtype=torch.uint8, device="cuda")
+    capacity = np.full(units, slots, np.int32)
+    handle = ss.ss_cache_create(B, hkv, np.zeros(B, np.int32), capacity, rec)
+    keys, vals = [np.zeros((0, hkv, D), np.float32)] * B, [np.zeros((0, hkv, D), np.float32)] * B
+    missed = 0
+    try:
+        for step, n_new in enumerate([[11 * blk + 3, 2 * blk - 1, 9 * blk], [1, 1, 1], [blk + 2, 1, 4 * blk], [1] * 3, [1] * 3]):
+            n = sum(n_new)
+            nk, nv = values(rng, n, hkv, D), values(rng, n, hkv, D)
+            new = to_bf16(np.stack([nk, nv], 2))
+            begin = np.concatenate([[0], np.cumsum(n_new)])
+            pos = np.concatenate([len(keys[b]) + np.arange(n_new[b]) for b in range(B)])
+            base = new.data_ptr()
+            at = dev(pos)  # block j of a unit is record j of its region: slots are positions
+            ss.ss_write_kv8(base, base + 2 * D, hkv * 4 * D, 4 * D, dev(begin), at, at, B, hkv, blk, D, n, fmt, mapped,
+                            pool_off, room, open_blocks, meta, 0, room)
+            for b in range(B):
+                keys[b] = np.concatenate([keys[b], nk[begin[b]:begin[b + 1]]])
+                vals[b] = np.concatenate([vals[b], nv[begin[b]:begin[b + 1]]])
+            nblk = np.array([len(x) // blk for x in keys], np.int32)
+            ss.ss_cache_set_blocks(handle, nblk)
+            q = ref.bf16(rng.standard_normal((B, hkv * G, D)))
+            d_q, d_nblk = to_bf16(q), dev(nblk)
+            scores, sel = torch.zeros(B, hkv, room, device="cuda"), empty(B, hkv, k)
+            ss.ss_score_topk(d_q, meta, d_nblk, B, hkv * G, hkv, room, D, k, scores, sel)
+            sel = host(sel)
+            slot, miss = np.zeros((B, hkv, k), np.int32), np.zeros((units * k, 4), np.int32)
+            n_miss = ss.ss_cache_resolve(handle, step, sel, k, slot, miss, units * k)
+            missed += n_miss
+            ss.ss_gather_blocks(dev(miss), n_miss, mapped, pool_off, cache, cache_off, d_nblk, dev(capacity), B, hkv, rec)
+            out = torch.zeros(B, hkv * G, D, device="cuda")
+            d_len = dev([len(x) for x in keys])
+            ss.ss_sparse_attention_kv8(d_q, cache, cache_off, dev(slot), None, 0, dev(capacity), slots, None, open_blocks,
+                                       d_len, fmt, B, hkv * G, hkv, D, blk, k, SCALE, out, None, 0)
+            out = host(out).astype(np.float64)
+            for b in range(B):
+                full = int(nblk[b])
+                tiles = [x[:full * blk].reshape(full, blk, hkv, D).transpose(2, 0, 1, 3) for x in (keys[b], vals[b])]
+                kk, vv = ref.unpack(ref.pack(*tiles, blk, fmt), blk, fmt)
+                for g in range(hkv):
+                    chosen = sel[b, g][sel[b, g] >= 0]
+                    assert len(chosen) == min(full, k)
+                    k_all = np.concatenate([kk[g, chosen].reshape(-1, D), keys[b][full * blk:, g].astype(np.float64)])
+                    v_all = np.concatenate([vv[g, chosen].reshape(-1, D), vals[b][full * blk:, g].astype(np.float64)])
+                    heads = slice(g * G, (g + 1) * G)
+                    want, bound = ref.attention(q[b, heads].astype(np.float64), k_all, v_all, SCALE)
+                    assert (np.abs(out[b, heads] - want) <= bound).all(), (step, b, g)
+        assert 0 < missed < 5 * units * k
+    finally:
+        torch.cuda.synchronize()
+        ss.ss_cache_destroy(handle)
+        ss.ss_host_free(addr)

@@ -208,3 +208,13 @@ def test_plain_attention_and_its_bound():
     less, _ = ref.attention(q, k[:-1], v[:-1], 1 / np.sqrt(128))
     assert (np.abs(less - out) > bound).any()
     assert (ref.attention(q, k[:0], v[:0], 1.0)[0] == 0).all()
+
+
+def test_gather_takes_both_kinds_of_record():
+    """Record sizes of bf16 and of 8 bits, no other; with no rows nothing is enqueued."""
+    args = [FAKE, 0, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, 1, 1]
+    for blk in (8, 16, 32):
+        ss.ss_gather_blocks(*args, 512 * blk, 0)
+        ss.ss_gather_blocks(*args, ref.record_bytes(blk), 0)
+    for size in (256 * 8, 256 * 16 + 64, 512 * 64, ref.record_bytes(8) + 16):
+        expect(UNSUPPORTED, ss.ss_gather_blocks, *args, size, 0)
