@@ -485,7 +485,10 @@ ss_status ss_read_kv8(const void *kv_base, const int64_t *region_off, const int3
  * open_blocks and len (device int32 [B]; both or neither): the len[b] % blk
  * tokens of the open record are attended too, in bf16.  With no token the
  * output is 0.  fp32 accumulation; codes and open tokens enter the products
- * exactly, probabilities with 24 bits.
+ * exactly, queries but for what lies 2^-38 below a head's largest, and
+ * probabilities with 23 bits, down to 2^-35 of the largest (a token of smaller
+ * weight than that counts as 0; the V scales of a unit weigh in, so one tile
+ * is weighed so beside the unit's largest).
  *   q: device bf16 [B][Hq][d], out: device fp32 [B][Hq][d]
  *   workspace: device, 4-byte aligned; a smaller one than
  *   ss_sparse_attention_kv8_workspace (or NULL) is taken with fewer splits

@@ -4,21 +4,30 @@
 //
 // As in attention.hip the query heads of a KV head are the 16 columns of the
 // matrix products.  A wave takes 32 tokens (8 KiB of codes) a step:
-//   S^T[2 x 16 tok x 16 heads] = K * Q^T     2 x 4 v_mfma_f32_16x16x32_bf16
-//   O^T[128 ch x 16 heads]    += V^T * P^T   8 x 3 v_mfma_f32_16x16x32_bf16
-// e4m3 and int8 codes are exact in bf16, so they are widened in registers and
-// the tiles' scales go where they cost one multiplication a token: K's into
-// the logit, V's into the probability.  P then enters the product as three
-// bf16 parts, 8 bits each, which keep all 24 of it.
+//   S^T[2 x 16 tok x 16 heads] = K * Q^T     2 x 4 v_mfma_f32_16x16x32_f16
+//   O^T[128 ch x 16 heads]    += V^T * P^T   8 x 2 v_mfma_f32_16x16x32_f16
+// e4m3 and int8 codes are exact in f16, so they are widened in registers (int8
+// by putting the byte into the low bits of 1024 + 128 + code) and the tiles'
+// scales go where they cost one multiplication a token: K's into the logit, V's
+// into the probability.  Queries become f16 by a power of two for each head,
+// which keeps bf16's 8 bits; p * scale enters as two f16 parts, by a power of two
+// for the wave's largest V scale, which keep 23 bits of it.  (With bf16 operands
+// and three parts a step took 211 vector instructions, e4m3, and 340, int8; now
+// 126 and 222: 11 requests of 512 selected blocks of 8 17.4 us, now 16.4; 64 x
+// 128 blocks 47.2, now 45.6.)
+// The maximum that p is relative to stays as it is until a logit passes it by
+// more than kLag, so that most steps exchange nothing between lanes.
 // The record's order of codes (kv8.hpp) makes a load instruction 1 KiB of
 // consecutive bytes and leaves each lane with its own operand bytes, so
-// nothing passes through LDS or between lanes:
+// nothing passes through LDS either:
 //   lane (L = lane/16, col = lane%16) holds K of token `col` of a subtile,
 //   16 channels a load; its accumulators are tokens 4L .. 4L+3 of both
 //   subtiles, and those tokens' codes are its V operand, channels 8*col + t.
 //
 // HBM bounds it (256 bytes and a share of the trailer a token and head).  Each
-// wave keeps two steps in flight.  Pages are resolved 64 entries at a time, an
+// wave keeps two steps in flight; a CU has about 40 KB of loads in flight
+// whatever the waves ask for (3 or 4 steps in flight gain nothing), so what
+// counts is that all CUs have work.  Pages are resolved 64 entries at a time, an
 // entry a lane, one set ahead, and read out as scalars.  A skipped entry reads
 // a record of zeros, so the loads are unconditional; offsets are 64 bits.
 //
@@ -39,13 +48,18 @@ constexpr int WAVES = 4;
 constexpr int CUS = 256;
 constexpr int kShares = 512;  // workgroups of SHARE, two a CU
 constexpr int kShareUnits = 40, kShareSteps = 512;  // from which they share (plan())
+constexpr float kNone = -3e38f;  // the maximum of no tokens
+constexpr float kLag = 4.f;       // p may grow to 2^kLag before its maximum is taken anew,
+constexpr float kMostV = 2048.f;  // V scales times gain to this: their product stays within 2^15, in f16's range
 constexpr int kMaxSplits = 256;
 constexpr int kMaxPartials = 4096;  // units * splits, where there is more than one split
 
 typedef unsigned int u32x4_t __attribute__((ext_vector_type(4)));
 typedef unsigned int u32x2_t __attribute__((ext_vector_type(2)));
 typedef float f32x2_t __attribute__((ext_vector_type(2)));
-typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+typedef float f4_t __attribute__((ext_vector_type(4), aligned(4)));  // the caller's floats
+typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
 
 // Records are addressed as global memory explicitly: where the compiler lost
 // that, it would wait for all loads in flight, the next step's among them.
@@ -64,25 +78,48 @@ __device__ __forceinline__ T load(gptr_t p)
 // what a skipped entry reads
 __device__ __align__(128) unsigned char zero_record[ss::kv8_record(32)];
 
-union frag_t {  // 8 x bf16
+union frag_t {  // 8 x bf16 or f16
     bf16x8_t v;
+    f16x8_t h;
     uint32_t w[4];
     u32x4_t u;
 };
 
-// four codes -> two registers of bf16 (exact)
+// four codes -> two registers of f16 (exact)
 template <int FMT>
 __device__ __forceinline__ void widen4(uint32_t c, uint32_t &a, uint32_t &b)
 {
     if constexpr (FMT == SS_KV8_E4M3) {
-        a = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c, 1.0f, false));
-        b = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c, 1.0f, true));
+        a = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(c, 1.0f, false));
+        b = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(c, 1.0f, true));
     } else {
-        const float x = (float)(int8_t)c, y = (float)(int8_t)(c >> 8), z = (float)(int8_t)(c >> 16), w = (float)(int8_t)(c >> 24);
-        a = __builtin_amdgcn_perm(__float_as_uint(y), __float_as_uint(x), 0x07060302);
-        b = __builtin_amdgcn_perm(__float_as_uint(w), __float_as_uint(z), 0x07060302);
+        // the bytes 128 + code become the low bits of 1024 + 128 + code
+        const f16x2_t off = {(_Float16)-1152.f, (_Float16)-1152.f};
+        c ^= 0x80808080u;
+        a = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2_t, __builtin_amdgcn_perm(0x64646464u, c, 0x04010400)) + off);
+        b = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2_t, __builtin_amdgcn_perm(0x64646464u, c, 0x04030402)) + off);
     }
 }
+
+// x minus the lower or upper f16 of h
+__device__ __forceinline__ float minus_lo(uint32_t h, float x)
+{
+    asm("v_fma_mix_f32 %0, %1, -1.0, %0 op_sel_hi:[1,0,0]" : "+v"(x) : "v"(h));
+    return x;
+}
+__device__ __forceinline__ float minus_hi(uint32_t h, float x)
+{
+    asm("v_fma_mix_f32 %0, %1, -1.0, %0 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "+v"(x) : "v"(h));
+    return x;
+}
+// two floats as f16, rounded to nearest even
+__device__ __forceinline__ uint32_t pack_f16(float x, float y)
+{
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2_t{x, y}, f16x2_t));
+}
+
+// 1/x of a power of two between 2^-126 and 2^126
+__device__ __forceinline__ float inverse(float x) { return __uint_as_float((254u << 23) - __float_as_uint(x)); }
 
 // maximum over the four 16-lane rows, in every lane
 __device__ __forceinline__ float rows_max(float x)
@@ -212,8 +249,9 @@ __global__ __launch_bounds__(WAVES * 64, MODE == SPLIT ? 3 : 2) void attn_kv8_ke
     constexpr int REC = ss::kv8_record(BLK), OPEN = 2 * BLK * D * 2;
     constexpr int EPS = TOK / BLK;        // entries of a step
     constexpr int SET = 64 / EPS;         // steps of a set of 64 entries
-    __shared__ float sm_m[WAVES][16], sm_l[WAVES][16];
-    __shared__ __align__(16) float sm_o[WAVES][16][D + 4];
+    // the waves' partial results, and that of the open record
+    __shared__ float sm_m[WAVES + 1][16], sm_l[WAVES + 1][16], sm_g[WAVES + 1];
+    __shared__ __align__(16) float sm_o[WAVES + 1][16][D + 4];
 
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -258,7 +296,8 @@ __global__ __launch_bounds__(WAVES * 64, MODE == SPLIT ? 3 : 2) void attn_kv8_ke
 #pragma unroll
         for (int m = 0; m < 4; ++m) {
             const int h = col < a.G ? col : 0;
-            const u32x4_t w = *reinterpret_cast<const u32x4_t *>(a.q + ((int64_t)b * a.Hq + g * a.G + h) * D + 64 * (m >> 1) + 16 * L + 8 * (m & 1));
+            const uint16_t *qh = a.q + ((int64_t)b * a.Hq + g * a.G + h) * D;
+            const u32x4_t w = *reinterpret_cast<const u32x4_t *>(qh + 64 * (m >> 1) + 16 * L + 8 * (m & 1));
             qf[m].u = col < a.G ? w : u32x4_t{0, 0, 0, 0};
         }
 
@@ -278,60 +317,29 @@ __global__ __launch_bounds__(WAVES * 64, MODE == SPLIT ? 3 : 2) void attn_kv8_ke
             return st < s_end && e < n_entries && block < blocks && page < limit ? page : -1;
         };
 
-        float mrun = -INFINITY, lrun = 0.f;
+        // Softmax state of head `col`: mref, the maximum that p is relative to;
+        // lrun, the lane's sum of p; gain, a power of two that the V scales are
+        // multiplied by, so that p * scale is in f16's range.
+        float mref = kNone, lrun = 0.f, gain = 0x1p126f;
         f32x4_t o[8];
 #pragma unroll
         for (int t = 0; t < 8; ++t) o[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-
-        // logits z (exp2 domain, -inf where masked) of the lane's tokens 4L + i of
-        // both subtiles, V scales and operand: one online softmax step
-        auto attend = [&](const float (&z)[8], float sv0, float sv1, auto &&vfrag) {
-            float cm = fmaxf(fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3])), fmaxf(fmaxf(z[4], z[5]), fmaxf(z[6], z[7])));
-            cm = rows_max(cm);
-            const float mnew = fmaxf(mrun, cm);
-            const float m0 = mnew == -INFINITY ? 0.f : mnew;  // nothing yet: every p is 0
-            if (__builtin_expect(__any(mnew != mrun), 0)) {
-                const float alpha = __builtin_amdgcn_exp2f(mrun - m0);
-#pragma unroll
-                for (int t = 0; t < 8; ++t) o[t] *= alpha;
-                lrun *= alpha;
-                mrun = mnew;
+        // a partial result to LDS; the lane holds channels 32L + 8i + t of head `col`
+        auto put = [&](int place) {
+            float l = lrun + __shfl_xor(lrun, 16);
+            l += __shfl_xor(l, 32);
+            if (L == 0) {
+                sm_m[place][col] = mref;
+                sm_l[place][col] = l;
             }
-            frag_t p1, p2, p3;
+            if (lane == 0) sm_g[place] = inverse(gain);
+            if (col < a.G) {
 #pragma unroll
-            for (int i = 0; i < 8; i += 2) {
-                float x[2];
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const float p = __builtin_amdgcn_exp2f(z[i + h] - m0);
-                    lrun += p;
-                    x[h] = p * (i < 4 ? sv0 : sv1);
+                for (int i = 0; i < 4; ++i) {
+                    float *row = &sm_o[place][col][32 * L + 8 * i];
+                    *reinterpret_cast<f32x4_t *>(row) = f32x4_t{o[0][i], o[1][i], o[2][i], o[3][i]};
+                    *reinterpret_cast<f32x4_t *>(row + 4) = f32x4_t{o[4][i], o[5][i], o[6][i], o[7][i]};
                 }
-                // three parts by truncation: each takes the upper half of what is left
-                auto upper = [&] { return __builtin_amdgcn_perm(__float_as_uint(x[1]), __float_as_uint(x[0]), 0x07060302); };
-                auto drop = [&](uint32_t w) {
-                    x[0] -= __uint_as_float(w << 16);
-                    x[1] -= __uint_as_float(w & 0xFFFF0000u);
-                };
-                p1.w[i >> 1] = upper();
-                drop(p1.w[i >> 1]);
-                p2.w[i >> 1] = upper();
-                drop(p2.w[i >> 1]);
-                p3.w[i >> 1] = upper();
-            }
-            // four accumulators in turn, so that none waits for its last product
-#pragma unroll
-            for (int t = 0; t < 8; t += 4) {
-                frag_t v[4];
-#pragma unroll
-                for (int h = 0; h < 4; ++h) v[h] = vfrag(t + h);
-#pragma unroll
-                for (int h = 0; h < 4; ++h) o[t + h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[h].v, p1.v, o[t + h], 0, 0, 0);
-#pragma unroll
-                for (int h = 0; h < 4; ++h) o[t + h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[h].v, p2.v, o[t + h], 0, 0, 0);
-#pragma unroll
-                for (int h = 0; h < 4; ++h) o[t + h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[h].v, p3.v, o[t + h], 0, 0, 0);
-                __builtin_amdgcn_sched_barrier(0);
             }
         };
 
@@ -377,8 +385,8 @@ __global__ __launch_bounds__(WAVES * 64, MODE == SPLIT ? 3 : 2) void attn_kv8_ke
                 }
             }
         };
+        float q_scale = 0.f;  // turns the products of f16 queries into logits (exp2 domain)
         auto compute_step = [&](const step_t &x) {
-            float z[8];
             f32x4_t acc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
             for (int m = 0; m < 4; ++m)
@@ -387,24 +395,67 @@ __global__ __launch_bounds__(WAVES * 64, MODE == SPLIT ? 3 : 2) void attn_kv8_ke
                     frag_t f;
                     widen4<FMT>(x.k[2 * s + (m >> 1)][2 * (m & 1)], f.w[0], f.w[1]);
                     widen4<FMT>(x.k[2 * s + (m >> 1)][2 * (m & 1) + 1], f.w[2], f.w[3]);
-                    acc[s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f.v, qf[m].v, acc[s], 0, 0, 0);
+                    acc[s] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f.h, qf[m].h, acc[s], 0, 0, 0);
+                }
+            const float sk[2] = {x.ok[0] ? x.sc[0].x * q_scale : 0.f, x.ok[1] ? x.sc[1].x * q_scale : 0.f};
+            float p[8], sv[2];  // logits relative to mref, then probabilities; V scales times gain
+            auto relate = [&] {
+#pragma unroll
+                for (int s = 0; s < 2; ++s) {
+                    const float bias = x.ok[s] ? -mref : -INFINITY;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) p[4 * s + i] = __builtin_fmaf(acc[s][i], sk[s], bias);
+                    sv[s] = x.sc[s].y * gain;
+                }
+                return fmaxf(fmaxf(fmaxf(p[0], p[1]), fmaxf(p[2], p[3])), fmaxf(fmaxf(p[4], p[5]), fmaxf(p[6], p[7])));
+            };
+            const float top = relate();
+            if (__builtin_expect(__any(top > kLag || fmaxf(sv[0], sv[1]) > kMostV), 0)) {
+                float z = -INFINITY, v = fmaxf(x.sc[0].y, x.sc[1].y);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) z = fmaxf(z, x.ok[i >> 2] ? acc[i >> 2][i & 3] * sk[i >> 2] : -INFINITY);
+                const float mnew = fmaxf(mref, rows_max(z));
+                if (BLK == 8) v = rows_max(v);
+                // the largest scale to [1024, 2048)
+                const float gnew = v * gain > kMostV ? __uint_as_float((uint32_t)min(254 + 10 - (int)(__float_as_uint(v) >> 23), 253) << 23) : gain;
+                const float alpha = __builtin_amdgcn_exp2f(mref - mnew), f = alpha * (gnew * inverse(gain));
+#pragma unroll
+                for (int t = 0; t < 8; ++t) o[t] *= f;
+                lrun *= alpha;
+                mref = mnew;
+                gain = gnew;
+                relate();
+            }
+            frag_t hi, lo;
+#pragma unroll
+            for (int i = 0; i < 8; i += 2) {
+                const float p0 = __builtin_amdgcn_exp2f(p[i]), p1 = __builtin_amdgcn_exp2f(p[i + 1]);
+                lrun += p0;
+                lrun += p1;
+                const float x0 = p0 * sv[i >> 2], x1 = p1 * sv[i >> 2];
+                hi.w[i >> 1] = pack_f16(x0, x1);
+                lo.w[i >> 1] = pack_f16(minus_lo(hi.w[i >> 1], x0), minus_hi(hi.w[i >> 1], x1));
+            }
+            // four accumulators in turn, so that none waits for its last product
+#pragma unroll
+            for (int t = 0; t < 8; t += 4) {
+                frag_t v[4];
+#pragma unroll
+                for (int h = 0; h < 4; ++h) {
+                    widen4<FMT>(x.v[t >> 2][h], v[h].w[0], v[h].w[1]);
+                    widen4<FMT>(x.v[2 + (t >> 2)][h], v[h].w[2], v[h].w[3]);
                 }
 #pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                const float sk = x.sc[s].x * a.scale_log2;
+                for (int h = 0; h < 4; ++h) o[t + h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v[h].h, hi.h, o[t + h], 0, 0, 0);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) z[4 * s + i] = x.ok[s] ? acc[s][i] * sk : -INFINITY;
+                for (int h = 0; h < 4; ++h) o[t + h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v[h].h, lo.h, o[t + h], 0, 0, 0);
+                __builtin_amdgcn_sched_barrier(0);
             }
-            attend(z, x.sc[0].y, x.sc[1].y, [&](int t) {
-                frag_t f;
-                widen4<FMT>(x.v[t >> 2][t & 3], f.w[0], f.w[1]);
-                widen4<FMT>(x.v[2 + (t >> 2)][t & 3], f.w[2], f.w[3]);
-                return f;
-            });
         };
 
         int st = s_begin + wave;
-        int pages = resolve(st), ahead = resolve(st + SET * WAVES);
+        int pages = resolve(st), ahead = -1;
+        if (s_end - s_begin > SET * WAVES) ahead = resolve(st + SET * WAVES);
         int at = 0, later = st + 2 * SET * WAVES;  // the next step's place in the set; the set after `ahead`
         auto load_next = [&](step_t &x) {
             int page[EPS];
@@ -423,10 +474,11 @@ __global__ __launch_bounds__(WAVES * 64, MODE == SPLIT ? 3 : 2) void attn_kv8_ke
         load_next(bufA);
 
         if (tail && wave == WAVES - 1) {
-            // the open record: bf16 rows of K, channel-major V, tokens past the last not read
+            // the open record, a partial result of its own: bf16 rows of K,
+            // channel-major V, and p as three bf16 parts; rows past the last are not read
             const uint8_t *ok = a.open + (int64_t)u * OPEN;
             const uint16_t *ov = reinterpret_cast<const uint16_t *>(ok + BLK * D * 2);
-            float z[8];
+            float z[8], cm = kNone;
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
                 f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
@@ -439,9 +491,29 @@ __global__ __launch_bounds__(WAVES * 64, MODE == SPLIT ? 3 : 2) void attn_kv8_ke
                     acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f.v, qf[m].v, acc, 0, 0, 0);
                 }
 #pragma unroll
-                for (int i = 0; i < 4; ++i) z[4 * s + i] = 16 * s + 4 * L + i < open_rows ? acc[i] * a.scale_log2 : -INFINITY;
+                for (int i = 0; i < 4; ++i) {
+                    z[4 * s + i] = 16 * s + 4 * L + i < open_rows ? acc[i] * a.scale_log2 : -INFINITY;
+                    cm = fmaxf(cm, z[4 * s + i]);
+                }
             }
-            attend(z, 1.f, 1.f, [&](int t) {
+            mref = rows_max(cm);
+            gain = 1.f;
+            frag_t part[3];
+#pragma unroll
+            for (int i = 0; i < 8; i += 2) {
+                float x0 = __builtin_amdgcn_exp2f(z[i] - mref), x1 = __builtin_amdgcn_exp2f(z[i + 1] - mref);
+                lrun += x0;
+                lrun += x1;
+#pragma unroll
+                for (int j = 0; j < 3; ++j) {  // each takes the upper half of what is left
+                    const uint32_t w = __builtin_amdgcn_perm(__float_as_uint(x1), __float_as_uint(x0), 0x07060302);
+                    part[j].w[i >> 1] = w;
+                    x0 -= __uint_as_float(w << 16);
+                    x1 -= __uint_as_float(w & 0xFFFF0000u);
+                }
+            }
+#pragma unroll
+            for (int t = 0; t < 8; ++t) {
                 frag_t f;
 #pragma unroll
                 for (int s = 0; s < 2; ++s) {
@@ -451,8 +523,39 @@ __global__ __launch_bounds__(WAVES * 64, MODE == SPLIT ? 3 : 2) void attn_kv8_ke
                     f.w[2 * s] = left > 1 ? w.x : w.x & 0xFFFFu;
                     f.w[2 * s + 1] = left > 3 ? w.y : left > 2 ? w.y & 0xFFFFu : 0u;
                 }
-                return f;
-            });
+#pragma unroll
+                for (int j = 0; j < 3; ++j) o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f.v, part[j].v, o[t], 0, 0, 0);
+            }
+            put(WAVES);
+            mref = kNone;
+            lrun = 0.f;
+            gain = 0x1p126f;
+#pragma unroll
+            for (int t = 0; t < 8; ++t) o[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        }
+
+        // the queries as f16, times a power of two that takes the head's largest
+        // to [2^14, 2^15): bf16's 8 bits fit, down to 2^-39 of the largest
+        {
+            uint32_t mag = 0;
+#pragma unroll
+            for (int m = 0; m < 4; ++m)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    mag = max(mag, max(qf[m].w[i] << 16 & 0x7FFF0000u, qf[m].w[i] & 0x7FFF0000u));
+            const int e = (int)(__float_as_uint(rows_max(__uint_as_float(min(mag, 0x7F800000u)))) >> 23);
+            const int to = min(254 + 14 - e, 253);
+            const float up = __uint_as_float((uint32_t)to << 23);
+            // with an infinity or a NaN among them every logit is NaN (and no skipped entry's)
+            const bool fine = e < 255;
+            q_scale = fine ? a.scale_log2 * inverse(up) : __uint_as_float(0x7FC00000u);
+#pragma unroll
+            for (int m = 0; m < 4; ++m)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t w = qf[m].w[i];
+                    qf[m].w[i] = fine ? pack_f16(__uint_as_float(w << 16) * up, __uint_as_float(w & 0xFFFF0000u) * up) : 0u;
+                }
         }
 
         for (; st < s_end; st += 2 * WAVES) {
@@ -462,48 +565,33 @@ __global__ __launch_bounds__(WAVES * 64, MODE == SPLIT ? 3 : 2) void attn_kv8_ke
             load_next(bufA);
             compute_step(bufB);
         }
-        lrun += __shfl_xor(lrun, 16);
-        lrun += __shfl_xor(lrun, 32);
-
-        // wave partials -> LDS; the lane holds channels 32L + 8i + t of head `col`
-        if (L == 0) {
-            sm_m[wave][col] = mrun;
-            sm_l[wave][col] = lrun;
-        }
-        if (col < a.G) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                float *row = &sm_o[wave][col][32 * L + 8 * i];
-                *reinterpret_cast<f32x4_t *>(row) = f32x4_t{o[0][i], o[1][i], o[2][i], o[3][i]};
-                *reinterpret_cast<f32x4_t *>(row + 4) = f32x4_t{o[4][i], o[5][i], o[6][i], o[7][i]};
-            }
-        }
+        put(wave);
         __syncthreads();
-        for (int idx = threadIdx.x; idx < a.G * D; idx += WAVES * 64) {
-            const int h = idx / D, ch = idx - h * D;
-            float M = sm_m[0][h];
-#pragma unroll
-            for (int w = 1; w < WAVES; ++w) M = fmaxf(M, sm_m[w][h]);
-            const float m0 = M == -INFINITY ? 0.f : M;
-            float lsum = 0.f, osum = 0.f;
-#pragma unroll
-            for (int w = 0; w < WAVES; ++w) {
-                const float sc = __builtin_amdgcn_exp2f(sm_m[w][h] - m0);
+        const int partials = tail ? WAVES + 1 : WAVES;
+        for (int idx = threadIdx.x; idx < a.G * (D / 4); idx += WAVES * 64) {
+            const int h = idx / (D / 4), ch = idx % (D / 4) * 4;
+            float M = kNone;
+            for (int w = 0; w < partials; ++w) M = fmaxf(M, sm_m[w][h]);
+            float lsum = 0.f;
+            f32x4_t osum = {0.f, 0.f, 0.f, 0.f};
+            for (int w = 0; w < partials; ++w) {
+                const float sc = __builtin_amdgcn_exp2f(sm_m[w][h] - M);
                 lsum += sc * sm_l[w][h];
-                osum += sc * sm_o[w][h][ch];
+                osum += sc * sm_g[w] * *reinterpret_cast<const f32x4_t *>(&sm_o[w][h][ch]);
             }
             if (first == 0 && last == nsteps) {
-                a.out[((int64_t)b * a.Hq + g * a.G) * D + idx] = lsum == 0.f ? 0.f : osum / lsum;
+                if (lsum != 0.f) osum /= lsum;
+                *reinterpret_cast<f4_t *>(a.out + ((int64_t)b * a.Hq + g * a.G + h) * D + ch) = osum;
             } else {
                 const int64_t place = MODE == SHARE ? (int64_t)blockIdx.x * 2 + (at_step == begin_step ? 0 : 1)
                                                     : (int64_t)u * gridDim.y + blockIdx.y;
                 float *pp = a.ws + (place * a.G + h) * kPartHead;
                 if (ch == 0) {
                     // a part that saw only NaN logits is kept: its sums are NaN
-                    pp[0] = M == -INFINITY && lsum != 0.f ? 0.f : M;
+                    pp[0] = M == kNone && lsum != 0.f ? 0.f : M;
                     pp[1] = lsum;
                 }
-                pp[2 + ch] = osum;
+                *reinterpret_cast<f4_t *>(pp + 2 + ch) = osum;
             }
         }
         if (MODE == SPLIT) return;

@@ -2,22 +2,28 @@
 the record's layout and its quantisation, the page bookkeeping row by row,
 and attention in 64 bits with a bound on what a kernel may be off.
 
-Bound of an attention output (n tokens, p the exact probabilities).  Codes
-and queries are exact in bf16, so a logit's products are exact and its error
-is that of an fp32 sum of 128 terms and of three roundings (the scale of the
-call, the tile's, their product): dz <= (128 * S + 4 * |z|) * u with S the
-sum of the terms' magnitudes (scaled) and u = 2^-24, and, for the rounded
-difference to the maximum, u * (|z| + |max|) more.  exp2 of the hardware is
-good to 2^-22.  Numerator and denominator each change by a factor within
-exp(+-dz) * (1 + 2^-22) and are fp32 sums of n terms and, between steps,
-waves and splits, some rescalings by exp2 (n + 64 roundings at most); the
-three bf16 parts keep 24 bits of p.  With A = sum p |v|:
+Bound of an attention output (n tokens, p the exact probabilities, u = 2^-24).
+Codes are exact in f16.  Queries are too but for what lies 2^-38 below the
+head's largest (scaled so that it is at least 2^14, and f16's last place is
+2^-24).  So a logit's products are exact up to that, and its error is that of
+an fp32 sum of 128 terms and of three roundings (the scale of the call, the
+tile's, their product): dz <= (128 * S + 4 * |z|) * u + 2^-38 * max|q| * K, with
+S the sum of the terms' magnitudes and K that of the key's (all scaled), and,
+for the rounded difference to the maximum, u * (|z| + |max|) more.  exp2 of
+the hardware is good to 2^-22.  Numerator and denominator each change by a
+factor within exp(+-dz) * (1 + 2^-22) and are fp32 sums of n terms and,
+between steps, waves and splits, some rescalings by exp2 (n + 64 roundings at
+most).  p times the tile's scale enters as two f16 parts, each rounded to
+nearest: 2^-23 of it.  With A = sum p |v|:
     |out - exact| <= A * (2 * dz + 2 * (n + 64) * u + 2^-20) + T.
-T is what fp32 cannot hold: a probability relative to the largest (the
-denominator is at least 1 there) below 2^-126 may count as 0, and so may a
-part of its product with the tile's scale, which then multiplies a code of
-at most 448.  Each of these costs a token at most 2^-126 * (|v| + 448), and
-there are four of them (p, and three parts): T = 4 * 2^-126 * sum (|v| + 448).
+T is what the formats cannot hold.  The f16 parts of a product end at 2^-25,
+where the scale of the largest V tile so far counts as 2^10 at least: a
+token loses at most 2^-35 of that scale times its code, 2^-35 of the largest
+|v|.  In fp32 (the open tokens' parts are bf16), a probability relative to
+the largest (the denominator is at least 1 there) below 2^-126 may count as
+0, and so may a part of its product with the tile's scale, which then
+multiplies a code of at most 448: a token loses at most 4 * 2^-126 *
+(|v| + 448).  T is the sum of both over the tokens.
 """
 import math
 
@@ -182,5 +188,6 @@ def attention(q, k, v, scale):
     p = np.exp(z - m)
     p /= p.sum(1, keepdims=True)
     dz = ((128 * mag + 4 * np.abs(z) + np.abs(z) + np.abs(m)).max(1, keepdims=True)) * U
-    lost = 4 * 2.0 ** -126 * (np.abs(v) + 448).sum(0)
+    dz += 2.0 ** -38 * np.abs(q).max(1, keepdims=True) * np.abs(k).sum(1).max() * abs(scale)
+    lost = len(k) * 2.0 ** -35 * np.abs(v).max() + 4 * 2.0 ** -126 * (np.abs(v) + 448).sum(0)
     return p @ v, (p @ np.abs(v)) * (2 * dz + 2 * (len(k) + 64) * U + 2.0 ** -20) + lost

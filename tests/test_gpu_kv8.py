@@ -625,6 +625,45 @@ def test_attention_large_logits(ss):
     s.check(attend(ss, s, None, 33), lambda b, g: range(33), False)
 
 
+def test_attention_of_queries_that_are_not_finite(ss):
+    """A head whose query holds an infinity or a NaN is NaN, the others of its
+    unit are not; where nothing is selected it is 0 all the same."""
+    rng = np.random.default_rng(51)
+    s = Stored(rng, 16, 0, [40 * 16 + 3, 16 * 5, 3], 2, 4)
+    s.q[0, 1, 77], s.q[0, 6, 0], s.q[1, 0, 5], s.q[2, 3, 1] = np.nan, np.inf, -np.inf, np.nan
+    s.to_device()
+    sel = rng.integers(-1, 41, (3, 2, 30)).astype(np.int32)
+    sel[1, 0] = -1  # nothing for the head with -inf
+    for chosen, k, with_open in ((sel, None, False), (None, 41, True)):
+        out = host(attend(ss, s, chosen, k, with_open=with_open))
+        nan = np.isnan(out)
+        want = np.zeros((3, 8), bool)
+        want[0, [1, 6]] = True
+        want[1, 0], want[2, 3] = chosen is None, chosen is None
+        assert np.array_equal(nan, np.broadcast_to(want[:, :, None], nan.shape))
+        if chosen is not None:
+            assert (out[1, :4] == 0).all() and (out[2] == 0).all()
+
+
+@pytest.mark.parametrize("fmt", [0, 1])
+def test_attention_of_scales_far_apart(ss, fmt):
+    """Tiles whose K and V scales differ by 2^24 within a unit, large ones
+    first, last and between; queries with channels 2^-30 of their largest."""
+    rng = np.random.default_rng(52)
+    for order in (1, -1):
+        s = Stored(rng, 16, fmt, [64 * 16, 64 * 16 + 9], 2, 4)
+        grow = np.exp2(np.linspace(-12, 12, s.n))[::order]
+        for g in range(2):
+            for page in range(s.n):
+                at = s.rec[g, page, 2 * 16 * D + 4:2 * 16 * D + 8].view(np.float32)
+                at *= np.float32(grow[page] if g else grow[rng.integers(s.n)])
+        s.q *= ref.bf16(np.exp2(rng.integers(-30, 1, s.q.shape)))
+        s.k, s.v = ref.unpack(s.rec, 16, fmt)
+        s.to_device()
+        s.check(attend(ss, s, None, 64, with_open=True), lambda b, g: range(64), True)
+        s.check(attend(ss, s, None, 64, with_open=True, room=0), lambda b, g: range(64), True)
+
+
 def test_results_repeat_and_streams(ss):
     """The same bits again, and on another stream than the current one."""
     rng = np.random.default_rng(50)
