@@ -86,7 +86,8 @@ ss_status ss_host_free(void *host_ptr);
 
 /* Measurement hook (not part of the method).  The next kernel that the
  * calling thread launches through this library -- the scoring, top-k,
- * gather, attention or metadata kernel of the next call that launches one;
+ * gather, attention or metadata kernel of the next call that launches one, or
+ * that of a call of the shared pool or the 8-bit cache;
  * for a split attention, its first kernel only; ss_score_topk scores and
  * selects rows of at most 256 blocks in one kernel where it can -- records `start_event`
  * (may be NULL) when it starts executing and `stop_event` (may be NULL)
@@ -490,9 +491,9 @@ ss_status ss_read_kv8(const void *kv_base, const int64_t *region_off, const int3
  * weight than that counts as 0; the V scales of a unit weigh in, so one tile
  * is weighed so beside the unit's largest).
  *   q: device bf16 [B][Hq][d], out: device fp32 [B][Hq][d]
- *   workspace: device, 4-byte aligned; a smaller one than
- *   ss_sparse_attention_kv8_workspace (or NULL) is taken with fewer splits
- *   and another order of the sums
+ *   workspace: device, 4-byte aligned, of calls that do not overlap; a smaller
+ *   one than ss_sparse_attention_kv8_workspace (or NULL) is taken with fewer
+ *   splits and another order of the sums.  Nothing in it outlives the call
  * k up to 65536.  Buffers 16-byte aligned. */
 size_t ss_sparse_attention_kv8_workspace(int B, int Hq, int Hkv, int d, int blk, int k);
 ss_status ss_sparse_attention_kv8(const void *q, const void *kv_base, const int64_t *region_off, const int32_t *sel,

@@ -146,7 +146,7 @@ def _ptr(x):
         pass
     if isinstance(x, int):
         return x
-    if hasattr(x, "__array_interface__"):  # numpy.ndarray
+    if hasattr(type(x), "ctypes"):  # numpy.ndarray (not a scalar)
         return x.__array_interface__["data"][0]
     raise TypeError(f"cannot pass {type(x)} as a buffer")
 

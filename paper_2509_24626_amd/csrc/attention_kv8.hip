@@ -587,8 +587,7 @@ __global__ __launch_bounds__(WAVES * 64, MODE == SPLIT ? 3 : 2) void attn_kv8_ke
                                                     : (int64_t)u * gridDim.y + blockIdx.y;
                 float *pp = a.ws + (place * a.G + h) * kPartHead;
                 if (ch == 0) {
-                    // a part that saw only NaN logits is kept: its sums are NaN
-                    pp[0] = M == kNone && lsum != 0.f ? 0.f : M;
+                    pp[0] = M;
                     pp[1] = lsum;
                 }
                 *reinterpret_cast<f4_t *>(pp + 2 + ch) = osum;
@@ -653,8 +652,9 @@ __global__ __launch_bounds__(W * 64) void join_kv8_kernel(const attn_args a, int
         M = mnew;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
+            // a part of weight 0 counts, for the NaN that it may hold
             const float sc = __uint_as_float(ss::lane_value(__float_as_uint(w), i));
-            if (sc != 0.f) {  // parts past the last weigh nothing, whatever they hold
+            if (p0 + i < parts) {
                 lsum += sc * __uint_as_float(ss::lane_value(__float_as_uint(ml.y), i));
                 osum.x += sc * x[i].x;
                 osum.y += sc * x[i].y;
@@ -702,7 +702,7 @@ struct split_plan {
 //
 // SPLIT takes the splits that cost least by a model of the time (us; fitted to
 // 1875 shapes of 1 to 1024 units, 1 to 4096 steps, G 1 to 16, each block size
-// and format: its choices lose 0.6% against the best on average, three
+// and format: its choices lose 0.8% against the best on average, three
 // workgroups a CU lose 5%, up to 50%):
 //   - the chip's bandwidth: kStepHbm a step;
 //   - the fullest CU: a workgroup's waves take a step each per round, of

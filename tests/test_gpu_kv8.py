@@ -616,6 +616,25 @@ def test_attention_of_a_tile_that_is_not_finite(ss, room):
     s.check(attend(ss, s, sel, room=room), lambda b, g: sel[b, g], False)
 
 
+@pytest.mark.parametrize("part", [0, 4])  # the K scale, the V scale
+@pytest.mark.parametrize("every", [False, True])
+def test_attention_keeps_a_nan_of_no_weight(ss, part, every):
+    """A NaN tile far below the others' logits, in another wave and another
+    split than theirs: its weight is 0 in fp32, its NaN stays."""
+    rng = np.random.default_rng(53)
+    B = 24 if every else 1
+    s = Stored(rng, 16, 0, [1200 * 16] + [16] * (B - 1), 2, 4)
+    s.q = ref.bf16(s.q * 0 + 300)  # a logit is the sum of a key's channels
+    low = s.tables[0, 700]
+    codes = s.rec[0, low, :16 * D]
+    codes[:] = (codes & 0x7F) | 0x80  # negative keys: the lowest logits
+    s.rec[0, low, 2 * 16 * D + part:2 * 16 * D + part + 4] = np.array([np.nan], np.float32).view(np.uint8)
+    s.to_device()
+    out = host(attend(ss, s, None, 1200, room=None))
+    nan = np.isnan(out)
+    assert nan[0, :4].all() and not nan[0, 4:].any() and not nan[1:].any()
+
+
 def test_attention_large_logits(ss):
     """Logits in the thousands: the maximum is taken out before exp."""
     rng = np.random.default_rng(49)

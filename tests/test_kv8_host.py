@@ -218,3 +218,12 @@ def test_gather_takes_both_kinds_of_record():
         ss.ss_gather_blocks(*args, ref.record_bytes(blk), 0)
     for size in (256 * 8, 256 * 16 + 64, 512 * 64, ref.record_bytes(8) + 16):
         expect(UNSUPPORTED, ss.ss_gather_blocks, *args, size, 0)
+
+
+def test_buffers_of_other_kinds_are_refused():
+    """What is no tensor, array or address is not taken for one (a numpy scalar has no address that lasts)."""
+    for x in (np.int64(4096), 1.5, "4096", [4096]):
+        with pytest.raises(TypeError):
+            ss.ss_block_release(*release_args(B=0, len=x))
+    for x in (True, 4096, np.zeros(4, np.int32), None):
+        ss.ss_block_release(*release_args(B=0, len=x))
