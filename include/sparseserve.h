@@ -391,7 +391,8 @@ ss_status ss_append_kv(const void *new_kv, int32_t *len_dev, int32_t *nblk_dev, 
  *   status: device int32 [B]: 0 served (also rows without new tokens); 1 the
  *       pool has too few pages: the first row whose pages, with all before,
  *       pass the pool and every later row that needs any; 2 the row would
- *       pass max_blocks; 3 a negative length, or token rows past token_cap.
+ *       pass max_blocks or 2^31 - 1 tokens; 3 a negative length, or token rows
+ *       past token_cap.
  *       A row that is not served takes nothing and keeps its length.
  * A page number outside the pool (in tables or free_pages) gives slots of -1.
  * B up to 65536; n_pages * blk below 2^31.  One launch up to 4096 token rows,
@@ -451,8 +452,8 @@ size_t ss_kv8_record_bytes(int blk, int d);
  *   meta: NULL, or the metadata of every block that fills, in meta_kind's
  *       layout with block capacity nblk_max, from the bf16 keys (the values
  *       of ss_build_metadata and ss_build_metadata_mean; the mean's fp64 sum
- *       may run in another order); then positions: device int32 [token_cap].
- *       Blocks at or above nblk_max get none
+ *       may run in another order), also where its page is out of range; then
+ *       positions: device int32 [token_cap].  Blocks at or above nblk_max get none
  * Buffers 16-byte aligned.  One launch. */
 ss_status ss_write_kv8(const void *k, const void *v, int64_t tok_stride, int64_t head_stride,
                        const int32_t *tok_begin, const int32_t *slots, const int32_t *positions, int B, int Hkv, int blk,
@@ -490,6 +491,8 @@ ss_status ss_read_kv8(const void *kv_base, const int64_t *region_off, const int3
  * probabilities with 23 bits, down to 2^-35 of the largest (a token of smaller
  * weight than that counts as 0; the V scales of a unit weigh in, so one tile
  * is weighed so beside the unit's largest).
+ * An infinity among the V values of an open token gives an infinity or NaN in
+ * its channel, in no other.
  *   q: device bf16 [B][Hq][d], out: device fp32 [B][Hq][d]
  *   workspace: device, 4-byte aligned, of calls that do not overlap; a smaller
  *   one than ss_sparse_attention_kv8_workspace (or NULL) is taken with fewer

@@ -118,7 +118,7 @@ __global__ __launch_bounds__(1024) void tables_kernel(const tables_args a)
         const uint32_t held = bad ? 0u : blocks_of((uint32_t)len, a.shift);
         const uint32_t after = bad ? 0u : blocks_of((uint32_t)len + nn, a.shift);
         const bool row_bad = bad || (nn > 0 && rows_end > cap);
-        const bool row_long = !row_bad && after > (uint32_t)a.max_blocks;
+        const bool row_long = !row_bad && (after > (uint32_t)a.max_blocks || (uint32_t)len + nn > 0x7FFFFFFFu);
         const uint32_t need = row_bad || row_long ? 0u : after - held;
         const uint32_t upto_w = wave_scan(need);
         if (lane == 63) s_need[wave] = upto_w;
@@ -422,7 +422,7 @@ extern "C" ss_status ss_block_tables(const int32_t *len, const int32_t *n_new, c
     ss::launch(one ? tables_kernel<true> : tables_kernel<false>, dim3(1), block, s, a);
     st = ss::check_launch("ss_block_tables");
     if (st != SS_OK || one) return st;
-    fill_rows_kernel<<<dim3((token_cap + kFillRows - 1) / kFillRows), dim3(256), 0, s>>>(a);
+    fill_rows_kernel<<<dim3((token_cap - 1) / kFillRows + 1), dim3(256), 0, s>>>(a);
     return ss::check_launch("ss_block_tables(rows)");
 }
 

@@ -145,7 +145,7 @@ class Pool:
             st, need = 0, 0
             if n_new[b] < 0 or have < 0 or (n and end > cap):
                 st = 3
-            elif self.held(have + n) > self.max_blocks:
+            elif self.held(have + n) > self.max_blocks or have + n > 2 ** 31 - 1:
                 st = 2
             else:
                 need = self.held(have + n) - self.held(have)

@@ -135,6 +135,25 @@ def test_tables_row_sums_past_32_bits(ss):
     t.reserve([3] + [2 ** 31 - 1] * 68 + [2], 64)
 
 
+@pytest.mark.parametrize("cap", [64, 5000])
+def test_tables_of_rows_near_the_largest_length(ss, cap):
+    """A length grows up to 2^31 - 1 and never past it."""
+    blk, top = 32, 2 ** 31 - 1
+    max_blocks = top // blk + 2  # so that the table is not what ends it
+    tables = empty(2, max_blocks, fill=3)
+    ln, nblk, n_free = dev([top - 8, top - 29]), empty(2), dev([4])
+    begin, taken, status, slots, pos = empty(3), empty(3), empty(2), empty(cap), empty(cap)
+    ss.ss_block_tables(ln, dev([20, 29]), n_free, 2, blk, max_blocks, 8, dev(np.arange(8)), tables, ln, nblk, n_free, begin,
+                       slots, pos, cap, taken, status)
+    assert host(status).tolist() == [2, 0] and host(ln).tolist() == [top - 8, top] and host(n_free)[0] == 4
+    assert host(begin).tolist() == [0, 20, 49] and host(taken).tolist() == [0, 0, 0]
+    assert host(nblk).tolist() == [(top - 8) // blk, top // blk]
+    where = np.concatenate([np.full(20, -1), np.arange(top - 29, top), np.full(cap - 49, -1)])
+    assert np.array_equal(host(pos), where)
+    assert np.array_equal(host(slots), np.where(where < 0, -1, 3 * blk + where % blk))
+    assert bool((tables == 3).all())
+
+
 def test_tables_bad_page_numbers(ss):
     """Page numbers outside the pool give slots of -1 and never an address."""
     rng = np.random.default_rng(13)
@@ -681,6 +700,44 @@ def test_attention_of_scales_far_apart(ss, fmt):
         s.to_device()
         s.check(attend(ss, s, None, 64, with_open=True), lambda b, g: range(64), True)
         s.check(attend(ss, s, None, 64, with_open=True, room=0), lambda b, g: range(64), True)
+
+
+def test_attention_of_infinite_open_values(ss):
+    """An infinity in an open V row: not finite in that channel, the others as
+    they are.  A probability enters in three bf16 parts, none negative: an
+    infinity times a positive one is infinite, times 0 (the last part of a
+    probability of 16 bits or fewer, such as 1) NaN."""
+    rng = np.random.default_rng(54)
+    s = Stored(rng, 16, 0, [5 * 16 + 7, 9], 2, 4)
+    s.open_v[0, 1, 3, 50], s.open_v[1, 0, 8, 127] = np.inf, -np.inf
+    s.to_device()
+    out = host(attend(ss, s, None, 6, with_open=True))
+    want = np.zeros(out.shape, bool)
+    want[0, 4:, 50], want[1, :4, 127] = True, True
+    assert np.array_equal(~np.isfinite(out), want)
+    s.open_v[0, 1, 3, 50], s.open_v[1, 0, 8, 127] = 0, 0  # the other channels by the formula
+    for b in range(2):
+        for g in range(2):
+            k, v = s.tokens(b, g, range(6), int(s.len[b]) % 16)
+            heads = slice(4 * g, 4 * g + 4)
+            plain, bound = ref.attention(s.q[b, heads].astype(np.float64), k, v, SCALE)
+            assert ((np.abs(out[b, heads] - plain) <= bound) | want[b, heads]).all()
+
+
+def test_two_streams_at_once(ss):
+    """Calls that overlap, each with its own workspace: the results of calls alone."""
+    rng = np.random.default_rng(55)
+    sets = [Stored(rng, 16, 0, [3000 * 16 + 3, 70 * 16], 2, 4).to_device(), Stored(rng, 8, 1, [2100 * 8] * 14, 3, 4).to_device()]
+    alone = [attend(ss, s, None, s.max_blocks, with_open=True) for s in sets]
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream(), torch.cuda.Stream()], [[], []]
+    for _ in range(6):
+        for i, s in enumerate(sets):
+            with torch.cuda.stream(streams[i]):
+                got[i].append(attend(ss, s, None, s.max_blocks, with_open=True))
+    torch.cuda.synchronize()
+    for want, results in zip(alone, got):
+        assert all(torch.equal(want, r) for r in results)
 
 
 def test_results_repeat_and_streams(ss):

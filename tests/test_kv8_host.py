@@ -173,6 +173,26 @@ def test_attention_takes_every_workspace_size():
     assert shared > 10
 
 
+ROWS = r"""
+P, got = 0x1000, []
+for cap in json.loads(sys.argv[2]):
+    ss.ss_block_tables(P, P, P, 3, 8, 100, 64, P, P, P, None, P, P, P, P, cap, P, P, stream=0)
+    got.append(launches())
+print(json.dumps(got))
+"""
+
+
+def test_tables_launch_all_token_rows():
+    """One workgroup up to 4096 token rows; beyond, a second launch covers them."""
+    import tempfile
+    stand_in = hip_stand_in.build(tempfile.mkdtemp()) or pytest.skip("no C compiler")
+    caps = [0, 1, 4096, 4097, 1 << 20, 2 ** 31 - 1024, 2 ** 31 - 1]
+    for cap, made in zip(caps, json.loads(hip_stand_in.run(stand_in, ROWS, json.dumps(caps)))):
+        assert made[0][:3] == [1, 1, 1] and len(made) == (1 if cap <= 4096 else 2)
+        if cap > 4096:
+            assert made[1][0] == -(-cap // 1024) and made[1][3] == 256
+
+
 def test_layout_is_a_permutation():
     for blk in (8, 16, 32):
         k, v = ref.places(blk)
