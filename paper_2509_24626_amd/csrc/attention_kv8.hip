@@ -417,7 +417,8 @@ __global__ __launch_bounds__(WAVES * 64, MODE == SPLIT ? 3 : 2) void attn_kv8_ke
                 const float mnew = fmaxf(mref, rows_max(z));
                 if (BLK == 8) v = rows_max(v);
                 // the largest scale to [1024, 2048)
-                const float gnew = v * gain > kMostV ? __uint_as_float((uint32_t)min(254 + 10 - (int)(__float_as_uint(v) >> 23), 253) << 23) : gain;
+                float gnew = gain;
+                if (v * gain > kMostV) gnew = __uint_as_float((uint32_t)min(254 + 10 - (int)(__float_as_uint(v) >> 23), 253) << 23);
                 const float alpha = __builtin_amdgcn_exp2f(mref - mnew), f = alpha * (gnew * inverse(gain));
 #pragma unroll
                 for (int t = 0; t < 8; ++t) o[t] *= f;
@@ -487,7 +488,8 @@ __global__ __launch_bounds__(WAVES * 64, MODE == SPLIT ? 3 : 2) void attn_kv8_ke
                     frag_t f;
                     f.u = u32x4_t{0, 0, 0, 0};
                     if (16 * s + col < open_rows)
-                        f.u = *reinterpret_cast<const u32x4_t *>(ok + (16 * s + col) * (D * 2) + (64 * (m >> 1) + 16 * L + 8 * (m & 1)) * 2);
+                        f.u = *reinterpret_cast<const u32x4_t *>(ok + (16 * s + col) * (D * 2) +
+                                                                 (64 * (m >> 1) + 16 * L + 8 * (m & 1)) * 2);
                     acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f.v, qf[m].v, acc, 0, 0, 0);
                 }
 #pragma unroll
@@ -724,7 +726,8 @@ split_plan plan(int64_t units, int k, int blk, int G, bool selected, size_t room
     for (int n = 1; n == 1 || (n <= most && n <= steps); ++n) {
         const int per = (steps + n - 1) / n, splits = (steps + per - 1) / per;
         if (n > 1 && splits < n) continue;  // the same as with fewer
-        const float groups = (float)units * splits, fullest = std::ceil(groups / CUS), rounds = (float)((per + WAVES - 1) / WAVES);
+        const float groups = (float)units * splits, fullest = std::ceil(groups / CUS);
+        const float rounds = (float)((per + WAVES - 1) / WAVES);
         const float hbm = all * kStepHbm;
         const float cu = rounds * (fullest == 1.f ? kRound1 : fullest == 2.f ? kRound2 : kRound3 * fullest) + kGroup * fullest;
         float cost = std::max(hbm, cu) + kBoth * std::min(hbm, cu);
@@ -754,7 +757,8 @@ template <int BLK>
 auto join_of(int mode, int waves)
 {
     if (mode == SHARE) return join_kv8_kernel<BLK, 8, SHARE>;
-    return waves == 1 ? join_kv8_kernel<BLK, 1, SPLIT> : waves == 4 ? join_kv8_kernel<BLK, 4, SPLIT> : join_kv8_kernel<BLK, 8, SPLIT>;
+    if (waves == 1) return join_kv8_kernel<BLK, 1, SPLIT>;
+    return waves == 4 ? join_kv8_kernel<BLK, 4, SPLIT> : join_kv8_kernel<BLK, 8, SPLIT>;
 }
 
 template <int FMT, int MODE>
@@ -772,7 +776,8 @@ extern "C" size_t ss_sparse_attention_kv8_workspace(int B, int Hq, int Hkv, int 
     const int64_t units = (int64_t)B * Hkv;
     const int G = Hq / Hkv;
     const size_t any = ~(size_t)0 >> 1;
-    return std::max(plan_bytes(plan(units, k, blk, G, false, any), units, G), plan_bytes(plan(units, k, blk, G, true, any), units, G));
+    return std::max(plan_bytes(plan(units, k, blk, G, false, any), units, G),
+                    plan_bytes(plan(units, k, blk, G, true, any), units, G));
 }
 
 extern "C" ss_status ss_sparse_attention_kv8(const void *q, const void *kv_base, const int64_t *region_off,
@@ -799,7 +804,8 @@ extern "C" ss_status ss_sparse_attention_kv8(const void *q, const void *kv_base,
     SS_CHECK_ARG((((uintptr_t)q | (uintptr_t)kv_base | (uintptr_t)open_blocks) & 15) == 0,
                  "ss_sparse_attention_kv8: buffers must be 16-byte aligned");
     const int64_t units = (int64_t)B * Hkv;
-    SS_CHECK_SUPPORTED(units <= 0x7FFFFFFF / (WAVES * 64), "ss_sparse_attention_kv8: %lld units pass the launch", (long long)units);
+    SS_CHECK_SUPPORTED(units <= 0x7FFFFFFF / (WAVES * 64), "ss_sparse_attention_kv8: %lld units pass the launch",
+                       (long long)units);
     const int G = Hq / Hkv;
     const split_plan sp = plan(units, k, blk, G, sel != nullptr, workspace ? ws_bytes : 0);
     const attn_args a = {static_cast<const uint16_t *>(q), static_cast<const uint8_t *>(kv_base), region_off, sel, tables,

@@ -54,7 +54,10 @@ __device__ __forceinline__ uint32_t wave_scan(uint32_t x)
 __device__ __forceinline__ uint32_t lane_of(uint32_t x, int lane) { return (uint32_t)__builtin_amdgcn_readlane((int)x, lane); }
 
 // what blocks of `blk` = 2^shift tokens n tokens take
-__device__ __forceinline__ uint32_t blocks_of(uint32_t n, int shift) { return (n >> shift) + ((n & ((1u << shift) - 1)) ? 1u : 0u); }
+__device__ __forceinline__ uint32_t blocks_of(uint32_t n, int shift)
+{
+    return (n >> shift) + ((n & ((1u << shift) - 1)) ? 1u : 0u);
+}
 
 struct row_t {
     int slot, pos;
@@ -106,7 +109,8 @@ __global__ __launch_bounds__(1024) void tables_kernel(const tables_args a)
         }
         const bool bad = len < 0 || n < 0;
         int open_page = -1;  // of the block that the row's tokens so far end in
-        if (FILL && !bad && live && (len >> a.shift) < a.max_blocks) open_page = a.tables[(int64_t)b * a.max_blocks + (len >> a.shift)];
+        if (FILL && !bad && live && (len >> a.shift) < a.max_blocks)
+            open_page = a.tables[(int64_t)b * a.max_blocks + (len >> a.shift)];
         const uint32_t nn = n < 0 ? 0u : (uint32_t)n;
         const uint32_t rows = wave_scan(nn);
         if (lane == 63) s_rows[wave] = rows;
@@ -159,7 +163,8 @@ __global__ __launch_bounds__(1024) void tables_kernel(const tables_args a)
                 int32_t *table = a.tables + (int64_t)b * a.max_blocks;
                 for (uint32_t r = begin; live && r < end; ++r) {
                     row_t x = {-1, -1};
-                    if (st == kServed) x = place_row((uint32_t)len + (r - begin), held, taken, open_page, a.n_pages, a.shift, table, page_of);
+                    if (st == kServed)
+                        x = place_row((uint32_t)len + (r - begin), held, taken, open_page, a.n_pages, a.shift, table, page_of);
                     a.slots[r] = x.slot;
                     if (a.positions) a.positions[r] = x.pos;
                 }
@@ -173,7 +178,8 @@ __global__ __launch_bounds__(1024) void tables_kernel(const tables_args a)
                     int32_t *table = a.tables + (int64_t)(b0 + wave * 64 + l) * a.max_blocks;
                     for (uint32_t r = begin_l + lane; r < end_l; r += 64) {
                         row_t x = {-1, -1};
-                        if (served) x = place_row(len_l + (r - begin_l), held_l, taken_l, open_l, a.n_pages, a.shift, table, page_of);
+                        if (served)
+                            x = place_row(len_l + (r - begin_l), held_l, taken_l, open_l, a.n_pages, a.shift, table, page_of);
                         a.slots[r] = x.slot;
                         if (a.positions) a.positions[r] = x.pos;
                     }

@@ -111,7 +111,10 @@ __device__ __forceinline__ u32x4_t load16_stream(const uint8_t *p)
 // Stores are streamed too: writing 64k tokens in blocks of 8 took 90.8 us with
 // the default policy, 74.9 so; reading 64k tokens 85.0 and 81.4.  It needs
 // whole lines (K codes stored 32 bytes at a time: 97.3).
-__device__ __forceinline__ void store16(uint8_t *p, u32x4_t x) { __builtin_nontemporal_store(x, reinterpret_cast<u32x4_t *>(p)); }
+__device__ __forceinline__ void store16(uint8_t *p, u32x4_t x)
+{
+    __builtin_nontemporal_store(x, reinterpret_cast<u32x4_t *>(p));
+}
 
 // Threads of a workgroup.  A team needs no other, and single waves leave and
 // are replaced soonest: writing 64k tokens of 8 heads with cuboids 74.4 us with
@@ -312,7 +315,8 @@ __global__ __launch_bounds__(kWriteThreads) void write_kernel(const write_args a
             const u32x4_t w = load16((r & 1 ? vh : kh) + (int64_t)(i0 + row) * a.tok_stride);
             if (r & 1) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) ov[(8 * x + e) * BLK + row] = (uint16_t)(e & 1 ? w[e >> 1] >> 16 : w[e >> 1] & 0xFFFFu);
+                for (int e = 0; e < 8; ++e)
+                    ov[(8 * x + e) * BLK + row] = (uint16_t)(e & 1 ? w[e >> 1] >> 16 : w[e >> 1] & 0xFFFFu);
             } else {
                 store16(open + row * (D * 2) + x * 16, w);
             }
@@ -419,7 +423,8 @@ __global__ __launch_bounds__(read_threads(BLK)) void read_kernel(const read_args
 #pragma unroll
             for (int h = 0; h < 2; ++h) {  // rows row + 2i + h
                 const bool mine = odd == (h == 1);
-                const u32x2_t lo = row4<FMT>(mine ? (odd ? w[2] : w[0]) : r0, sc.x), hi = row4<FMT>(mine ? (odd ? w[3] : w[1]) : r1, sc.x);
+                const u32x2_t lo = row4<FMT>(mine ? (odd ? w[2] : w[0]) : r0, sc.x);
+                const u32x2_t hi = row4<FMT>(mine ? (odd ? w[3] : w[1]) : r1, sc.x);
                 if (row + 2 * i + h < here)
                     store16(ko + (row + 2 * i + h) * a.row_stride, u32x4_t{lo.x, lo.y, hi.x, hi.y});
             }
@@ -498,7 +503,8 @@ extern "C" ss_status ss_write_kv8(const void *k, const void *v, int64_t tok_stri
     SS_CHECK_ARG(aligned16(k) && aligned16(v) && aligned16(kv_base) && aligned16(open_blocks) && aligned16(meta),
                  "ss_write_kv8: buffers must be 16-byte aligned");
     const int64_t teams = ((int64_t)B + token_cap / blk) * Hkv, groups = groups_of(teams, blk, kWriteThreads);
-    SS_CHECK_SUPPORTED(groups <= 0x7FFFFFFF / kWriteThreads, "ss_write_kv8: %lld block records pass the launch", (long long)teams);
+    SS_CHECK_SUPPORTED(groups <= 0x7FFFFFFF / kWriteThreads, "ss_write_kv8: %lld block records pass the launch",
+                       (long long)teams);
     const write_args a = {static_cast<const uint8_t *>(k), static_cast<const uint8_t *>(v), tok_stride, head_stride,
                           tok_begin, slots, positions, B, Hkv, token_cap, static_cast<uint8_t *>(kv_base), region_off,
                           slot_limit, static_cast<uint8_t *>(open_blocks), static_cast<uint8_t *>(meta), nblk_max, teams};
@@ -527,11 +533,12 @@ extern "C" ss_status ss_read_kv8(const void *kv_base, const int64_t *region_off,
     SS_CHECK_ARG(aligned16(kv_base) && aligned16(open_blocks) && aligned16(k) && aligned16(v),
                  "ss_read_kv8: buffers must be 16-byte aligned");
     const int64_t teams = ((int64_t)B + rows / blk) * Hkv, groups = groups_of(teams, blk, read_threads(blk));
-    SS_CHECK_SUPPORTED(groups <= 0x7FFFFFFF / read_threads(blk), "ss_read_kv8: %lld block records pass the launch", (long long)teams);
+    SS_CHECK_SUPPORTED(groups <= 0x7FFFFFFF / read_threads(blk), "ss_read_kv8: %lld block records pass the launch",
+                       (long long)teams);
     const read_args a = {static_cast<const uint8_t *>(kv_base), region_off, tables, max_blocks, slot_limit,
                          static_cast<const uint8_t *>(open_blocks), len, row_begin, B, Hkv, rows, static_cast<uint8_t *>(k),
                          static_cast<uint8_t *>(v), row_stride, head_stride, teams};
-    ss::launch(fmt == SS_KV8_E4M3 ? read_of<SS_KV8_E4M3>(blk) : read_of<SS_KV8_INT8>(blk), dim3((unsigned)groups), dim3(read_threads(blk)),
-               ss::as_stream(stream), a);
+    auto *kernel = fmt == SS_KV8_E4M3 ? read_of<SS_KV8_E4M3>(blk) : read_of<SS_KV8_INT8>(blk);
+    ss::launch(kernel, dim3((unsigned)groups), dim3(read_threads(blk)), ss::as_stream(stream), a);
     return ss::check_launch("ss_read_kv8");
 }
