@@ -147,35 +147,40 @@ __global__ __launch_bounds__(kWriteThreads) void write_kernel(const write_args a
     constexpr int NR = 4 * SUB;  // rows of a lane
     constexpr int REC = ss::kv8_record(BLK), OPEN = 2 * BLK * D * 2;
     const int lane = threadIdx.x & 63, tl = lane % TEAM, x = lane & 15, L = tl >> 4;
-    const int64_t team = ((int64_t)blockIdx.x * kWriteThreads + threadIdx.x) / TEAM;
-    const int64_t item = team / a.Hkv;
-    const int g = (int)(team - item * a.Hkv);
+    const uint32_t team = (blockIdx.x * kWriteThreads + threadIdx.x) / TEAM, item = team / (uint32_t)a.Hkv;
+    const int g = (int)(team - item * (uint32_t)a.Hkv);
     const int b = ss::find_item<BLK, TEAM>(a.tok_begin, a.B, item, lane);
+    const int64_t u = (int64_t)b * a.Hkv + g;
     const int tb = a.tok_begin[b], n = min(a.tok_begin[b + 1], a.token_cap) - tb;
-    const int64_t m64 = item - (b + (int64_t)(tb / BLK));
+    int64_t region = a.region_off[u];
+    const int64_t m64 = (int64_t)item - (b + (int64_t)(tb / BLK));
     if (team >= a.teams || tb < 0 || n <= 0 || m64 < 0 || m64 > n / BLK) return;  // the whole team
     const int s0 = a.slots[tb];
     if (s0 < 0) return;  // a sequence that found no pages
     const int m = (int)m64, p0 = s0 % BLK;
     const int full = (p0 + n) / BLK;  // blocks that fill
     if (m >= max(full, 1)) return;
-    const int64_t u = (int64_t)b * a.Hkv + g;
     uint8_t *open = a.open + u * OPEN;
     const uint8_t *kh = a.k + g * a.head_stride + x * 16, *vh = a.v + g * a.head_stride + x * 16;
 
     if (full > 0) {
         u32x4_t K[NR], V[NR];
         const int i0 = tb + m * BLK - p0;  // the token of the block's row 0
+        // where the block goes, beside its rows and not after them
+        int last = a.slots[i0 + BLK - 1], pos = META == kNoMeta ? 0 : a.positions[i0 + BLK - 1];
+        const int held = m == 0 ? p0 : 0;  // rows of the open record
+        const uint8_t *k0 = kh + (int64_t)(i0 + 4 * L) * a.tok_stride, *v0 = vh + (int64_t)(i0 + 4 * L) * a.tok_stride;
 #pragma unroll
         for (int r = 0; r < NR; ++r) {
             const int row = (r >> 2) * 16 + 4 * L + (r & 3);
-            const int64_t tok = max(i0 + row, tb);  // a row of the open record reads some new token, replaced below
-            const uint8_t *kp = kh + tok * a.tok_stride;
-            if (m == 0 && row < p0) kp = open + row * (D * 2) + x * 16;
+            const int64_t at = ((r >> 2) * 16 + (r & 3)) * a.tok_stride;
+            const uint8_t *kp = k0 + at, *vp = v0 + at;
+            if (row < held) kp = vp = open + row * (D * 2) + x * 16;  // V is replaced below
             K[r] = load16_stream(kp);
-            V[r] = load16_stream(vh + tok * a.tok_stride);
+            V[r] = load16_stream(vp);
         }
-        if (m == 0 && p0 > 0) {
+        asm volatile("" : "+v"(last), "+v"(pos), "+v"(region));
+        if (held > 0) {
             const uint8_t *ov = open + BLK * D * 2;
 #pragma unroll
             for (int s = 0; s < SUB; ++s) {
@@ -185,7 +190,7 @@ __global__ __launch_bounds__(kWriteThreads) void write_kernel(const write_args a
                     w[e] = *reinterpret_cast<const u32x2_t *>(ov + ((8 * x + e) * BLK + s * 16 + 4 * L) * 2);
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    if (s * 16 + 4 * L + i < p0) {
+                    if (s * 16 + 4 * L + i < held) {
 #pragma unroll
                         for (int h = 0; h < 4; ++h) {
                             const uint32_t lo = w[2 * h][i >> 1], hi = w[2 * h + 1][i >> 1];
@@ -206,9 +211,9 @@ __global__ __launch_bounds__(kWriteThreads) void write_kernel(const write_args a
         const uint32_t mm = team_max2<TEAM>(max2((mk & 0xFFFFu) | (mv << 16), (mk >> 16) | (mv & 0xFFFF0000u)));
         const tile_scale<FMT> sk(mm & 0xFFFFu), sv(mm >> 16);
 
-        const int last = a.slots[i0 + BLK - 1], page = last / BLK;
+        const int page = last / BLK;
         if (last >= 0 && page < a.slot_limit && last % BLK == BLK - 1) {
-            uint8_t *rec = a.kv + a.region_off[u] + (int64_t)page * REC;
+            uint8_t *rec = a.kv + region + (int64_t)page * REC;
 #pragma unroll
             for (int s = 0; s < SUB; ++s) {
                 uint8_t *kt = rec + s * T * D, *vt = rec + BLK * D + s * T * D;
@@ -239,6 +244,7 @@ __global__ __launch_bounds__(kWriteThreads) void write_kernel(const write_args a
                 }
                 constexpr int HALF = TEAM / 32;  // lane rows of half a team
                 uint8_t *kl = kt + (x >> 1) * (T * 16) + (4 * (L % HALF) + 2 * (L / HALF) + (odd ? 1 : 0)) * 16;
+                asm("" : "+v"(o[0]), "+v"(o[1]));  // else the two stores lose their policy on the way to the assembly
                 store16(kl, o[0]);
                 store16(kl + HALF * 64, o[1]);
 #pragma unroll
@@ -258,7 +264,6 @@ __global__ __launch_bounds__(kWriteThreads) void write_kernel(const write_args a
             }
         }
         if (META != kNoMeta) {
-            const int pos = a.positions[i0 + BLK - 1];
             const int jb = pos / BLK;
             const bool live = pos >= 0 && jb < a.nblk_max;
             if (META == SS_META_CUBOID) {
@@ -286,20 +291,41 @@ __global__ __launch_bounds__(kWriteThreads) void write_kernel(const write_args a
                 if (live && L == hi * (TEAM / 32))
                     store16(a.meta + (u * a.nblk_max + jb) * (int64_t)(4 * D) + hi * (2 * D) + x * 16, o);
             } else {
-                double sum[8];
+                // the team's lanes exchange, so that each sums all rows of its own 4 (a
+                // team of 64: 2) channels
+                constexpr int W = 64 / TEAM;  // words of two channels
+                uint32_t t[2 * NR][2], w[BLK][W];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    sum[e] = 0.0;
+                for (int r = 0; r < NR; ++r)
 #pragma unroll
-                    for (int r = 0; r < NR; ++r) sum[e] += (double)channel(K[r], e);
-                    sum[e] += __shfl_xor(sum[e], 16);
-                    if (TEAM == 64) sum[e] += __shfl_xor(sum[e], 32);
+                    for (int h = 0; h < 2; ++h) {
+                        const auto y = TEAM == 64 ? __builtin_amdgcn_permlane32_swap(K[r][h], K[r][2 + h], false, false)
+                                                  : __builtin_amdgcn_permlane16_swap(K[r][h], K[r][2 + h], false, false);
+                        t[2 * r][h] = y[0];
+                        t[2 * r + 1][h] = y[1];
+                    }
+#pragma unroll
+                for (int r = 0; r < 2 * NR; ++r) {
+                    if constexpr (TEAM == 64) {
+                        const auto y = __builtin_amdgcn_permlane16_swap(t[r][0], t[r][1], false, false);
+                        w[2 * r][0] = y[0];
+                        w[2 * r + 1][0] = y[1];
+                    } else {
+                        w[r][0] = t[r][0];
+                        w[r][1] = t[r][1];
+                    }
                 }
-                u32x4_t o;
+                uint8_t *mean = a.meta + (u * a.nblk_max + jb) * (int64_t)(2 * D) + x * 16 + L * (W * 4);
 #pragma unroll
-                for (int h = 0; h < 4; ++h) o[h] = ss::pack_bf16_rne_f64(sum[2 * h] * (1.0 / BLK), sum[2 * h + 1] * (1.0 / BLK));
-                if (live && L == 0)
-                    store16(a.meta + (u * a.nblk_max + jb) * (int64_t)(2 * D) + x * 16, o);
+                for (int h = 0; h < W; ++h) {
+                    double lo = 0.0, hi = 0.0;
+#pragma unroll
+                    for (int r = 0; r < BLK; ++r) {
+                        lo += (double)bf16_lo(w[r][h]);
+                        hi += (double)bf16_hi(w[r][h]);
+                    }
+                    if (live) reinterpret_cast<uint32_t *>(mean)[h] = ss::pack_bf16_rne_f64(lo * (1.0 / BLK), hi * (1.0 / BLK));
+                }
             }
         }
     }
@@ -369,16 +395,16 @@ __global__ __launch_bounds__(read_threads(BLK)) void read_kernel(const read_args
     constexpr int SUB = BLK == 32 ? 2 : 1, T = BLK / SUB;
     constexpr int REC = ss::kv8_record(BLK), OPEN = 2 * BLK * D * 2;
     const int lane = threadIdx.x & 63, tl = lane % TEAM, x = lane & 15, L = tl >> 4;
-    const int64_t team = ((int64_t)blockIdx.x * read_threads(BLK) + threadIdx.x) / TEAM;
-    const int64_t item = team / a.Hkv;
-    const int g = (int)(team - item * a.Hkv);
+    const uint32_t team = (blockIdx.x * read_threads(BLK) + threadIdx.x) / TEAM, item = team / (uint32_t)a.Hkv;
+    const int g = (int)(team - item * (uint32_t)a.Hkv);
     const int b = ss::find_item<BLK, TEAM>(a.row_begin, a.B, item, lane);
+    const int64_t u = (int64_t)b * a.Hkv + g;
     const int rb = a.row_begin[b], len = a.len[b];
+    int64_t region = a.region_off[u];
     const int n = min(min(a.row_begin[b + 1], a.rows) - rb, len);
-    const int64_t j64 = item - (b + (int64_t)(rb / BLK));
+    const int64_t j64 = (int64_t)item - (b + (int64_t)(rb / BLK));
     if (team >= a.teams || rb < 0 || n <= 0 || j64 < 0 || j64 > (n - 1) / BLK) return;
     const int j = (int)j64, here = min(n - j * BLK, BLK);  // rows of this block
-    const int64_t u = (int64_t)b * a.Hkv + g;
     const int64_t out0 = (int64_t)(rb + j * BLK) * a.row_stride + g * a.head_stride + x * 16;
     uint8_t *ko = a.k + out0, *vo = a.v + out0;
     if (j >= len / BLK) {  // the open record's rows
@@ -395,8 +421,9 @@ __global__ __launch_bounds__(read_threads(BLK)) void read_kernel(const read_args
     }
     int page = j;
     if (a.tables) page = j < a.max_blocks ? a.tables[(int64_t)b * a.max_blocks + j] : -1;
+    asm volatile("" : "+v"(region));  // loaded beside the table's entry, not after it
     const bool ok = page >= 0 && page < a.slot_limit;
-    const uint8_t *rec = a.kv + a.region_off[u] + (int64_t)(ok ? page : 0) * REC;
+    const uint8_t *rec = a.kv + region + (int64_t)(ok ? page : 0) * REC;
     u32x4_t K[2 * SUB], V[2 * SUB];
     f32x2_t sc = {0.f, 0.f};
 #pragma unroll
