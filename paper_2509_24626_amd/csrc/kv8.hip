@@ -12,11 +12,14 @@
 // each step one rounded fp32 operation, so that the result does not depend on
 // the shape of the launch.
 //
-// A team of 64 lanes (32 for blocks of 8) takes one block of one head: 16
+// A team of 64 lanes (32 for blocks of 8) writes one block of one head: 16
 // lanes read 256 B of a token, so K and V of the block are in its registers
 // with two loads per 4 tokens in flight each, the maxima of both are one
 // packed reduction, and the codes leave as 16-byte stores.  Teams of
 // neighbouring heads are neighbours, so that together they read whole tokens.
+// A team reads back at most 16 tokens of a block (with all of a block of 32 to
+// a team, 7 sequences of 5000 tokens, 2 heads, took 8.6 us, 6.8 so; one of 64k
+// tokens, 8 heads, 79 and 77).
 // HBM bounds it: 512 B in and 256 B (and 8 per token for the trailer at 16
 // tokens a block) out per token and head, and the block's metadata.
 #include <algorithm>
@@ -392,29 +395,31 @@ template <int BLK, int FMT>
 __global__ __launch_bounds__(read_threads(BLK)) void read_kernel(const read_args a)
 {
     constexpr int TEAM = BLK == 8 ? 32 : 64;
-    constexpr int SUB = BLK == 32 ? 2 : 1, T = BLK / SUB;
+    constexpr int SUB = BLK == 32 ? 2 : 1, T = BLK / SUB;  // a team reads a subtile
     constexpr int REC = ss::kv8_record(BLK), OPEN = 2 * BLK * D * 2;
     const int lane = threadIdx.x & 63, tl = lane % TEAM, x = lane & 15, L = tl >> 4;
     const uint32_t team = (blockIdx.x * read_threads(BLK) + threadIdx.x) / TEAM, item = team / (uint32_t)a.Hkv;
     const int g = (int)(team - item * (uint32_t)a.Hkv);
-    const int b = ss::find_item<BLK, TEAM>(a.row_begin, a.B, item, lane);
+    const int b = ss::find_item<T, TEAM>(a.row_begin, a.B, item, lane);
     const int64_t u = (int64_t)b * a.Hkv + g;
     const int rb = a.row_begin[b], len = a.len[b];
     int64_t region = a.region_off[u];
     const int n = min(min(a.row_begin[b + 1], a.rows) - rb, len);
-    const int64_t j64 = (int64_t)item - (b + (int64_t)(rb / BLK));
-    if (team >= a.teams || rb < 0 || n <= 0 || j64 < 0 || j64 > (n - 1) / BLK) return;
-    const int j = (int)j64, here = min(n - j * BLK, BLK);  // rows of this block
-    const int64_t out0 = (int64_t)(rb + j * BLK) * a.row_stride + g * a.head_stride + x * 16;
+    const int64_t i64 = (int64_t)item - (b + (int64_t)(rb / T));
+    if (team >= a.teams || rb < 0 || n <= 0 || i64 < 0 || i64 > (n - 1) / T) return;
+    const int i0 = (int)i64 * T, here = min(n - i0, T);  // rows from i0 on
+    const int j = i0 / BLK, s = SUB == 1 ? 0 : i0 % BLK / T;
+    const int64_t out0 = (int64_t)(rb + i0) * a.row_stride + g * a.head_stride + x * 16;
     uint8_t *ko = a.k + out0, *vo = a.v + out0;
     if (j >= len / BLK) {  // the open record's rows
         const uint8_t *open = a.open + u * OPEN;
         const uint16_t *ov = reinterpret_cast<const uint16_t *>(open + BLK * D * 2);
         for (int r = L; r < here; r += TEAM / 16) {
-            store16(ko + r * a.row_stride, load16(open + r * (D * 2) + x * 16));
+            const int p = s * T + r;
+            store16(ko + r * a.row_stride, load16(open + p * (D * 2) + x * 16));
             u32x4_t w;
 #pragma unroll
-            for (int h = 0; h < 4; ++h) w[h] = ov[(8 * x + 2 * h) * BLK + r] | (uint32_t)ov[(8 * x + 2 * h + 1) * BLK + r] << 16;
+            for (int h = 0; h < 4; ++h) w[h] = ov[(8 * x + 2 * h) * BLK + p] | (uint32_t)ov[(8 * x + 2 * h + 1) * BLK + p] << 16;
             store16(vo + r * a.row_stride, w);
         }
         return;
@@ -424,53 +429,48 @@ __global__ __launch_bounds__(read_threads(BLK)) void read_kernel(const read_args
     asm volatile("" : "+v"(region));  // loaded beside the table's entry, not after it
     const bool ok = page >= 0 && page < a.slot_limit;
     const uint8_t *rec = a.kv + region + (int64_t)(ok ? page : 0) * REC;
-    u32x4_t K[2 * SUB], V[2 * SUB];
+    u32x4_t K[2] = {}, V[2] = {};
     f32x2_t sc = {0.f, 0.f};
-#pragma unroll
-    for (int i = 0; i < 2 * SUB; ++i) K[i] = V[i] = u32x4_t{0, 0, 0, 0};
     if (ok) {
-#pragma unroll
-        for (int s = 0; s < SUB; ++s)
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                K[2 * s + i] = load16(rec + s * T * D + (x >> 1) * (T * 16) + (4 * L + 2 * i + (x & 1)) * 16);
-                V[2 * s + i] = load16(rec + BLK * D + s * T * D + i * (T * 64) + L * 256 + x * 16);
-            }
         sc = *reinterpret_cast<const f32x2_t *>(rec + 2 * BLK * D);
+        const uint8_t *kt = rec + s * T * D + (x >> 1) * (T * 16) + (4 * L + (x & 1)) * 16;
+        const uint8_t *vt = rec + BLK * D + s * T * D + L * 256 + x * 16;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) K[i] = load16(kt + i * 32);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) V[i] = load16(vt + i * (T * 64));
+    }
+    const int row = 4 * L;
+    ko += row * a.row_stride;
+    vo += row * a.row_stride;
+    // a lane holds 16 channels of one of two rows; the pair exchanges so that each has 8 of both
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const u32x4_t w = K[i];
+        const bool odd = x & 1;
+        const uint32_t r0 = ss::pair_swap(odd ? w[0] : w[2]), r1 = ss::pair_swap(odd ? w[1] : w[3]);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {  // rows row + 2i + h
+            const bool mine = odd == (h == 1);
+            const u32x2_t lo = row4<FMT>(mine ? (odd ? w[2] : w[0]) : r0, sc.x);
+            const u32x2_t hi = row4<FMT>(mine ? (odd ? w[3] : w[1]) : r1, sc.x);
+            if (row + 2 * i + h < here) store16(ko + (2 * i + h) * a.row_stride, u32x4_t{lo.x, lo.y, hi.x, hi.y});
+        }
+    }
+    u32x4_t o[4];
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) {  // channels 8x + e, 8x + e + 1
+        const uint32_t w0 = V[e >> 2][e & 3], w1 = V[e >> 2][(e & 3) + 1];
+        const f32x2_t a0 = values2<FMT, false>(w0), a1 = values2<FMT, true>(w0);
+        const f32x2_t b0 = values2<FMT, false>(w1), b1 = values2<FMT, true>(w1);
+        o[0][e >> 1] = pack2(a0.x * sc.y, b0.x * sc.y);
+        o[1][e >> 1] = pack2(a0.y * sc.y, b0.y * sc.y);
+        o[2][e >> 1] = pack2(a1.x * sc.y, b1.x * sc.y);
+        o[3][e >> 1] = pack2(a1.y * sc.y, b1.y * sc.y);
     }
 #pragma unroll
-    for (int s = 0; s < SUB; ++s) {
-        const int row = s * 16 + 4 * L;
-        // a lane holds 16 channels of one of two rows; the pair exchanges so that each has 8 of both
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const u32x4_t w = K[2 * s + i];
-            const bool odd = x & 1;
-            const uint32_t r0 = ss::pair_swap(odd ? w[0] : w[2]), r1 = ss::pair_swap(odd ? w[1] : w[3]);
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {  // rows row + 2i + h
-                const bool mine = odd == (h == 1);
-                const u32x2_t lo = row4<FMT>(mine ? (odd ? w[2] : w[0]) : r0, sc.x);
-                const u32x2_t hi = row4<FMT>(mine ? (odd ? w[3] : w[1]) : r1, sc.x);
-                if (row + 2 * i + h < here)
-                    store16(ko + (row + 2 * i + h) * a.row_stride, u32x4_t{lo.x, lo.y, hi.x, hi.y});
-            }
-        }
-        u32x4_t o[4];
-#pragma unroll
-        for (int e = 0; e < 8; e += 2) {  // channels 8x + e, 8x + e + 1
-            const uint32_t w0 = V[2 * s + (e >> 2)][e & 3], w1 = V[2 * s + (e >> 2)][(e & 3) + 1];
-            const f32x2_t a0 = values2<FMT, false>(w0), a1 = values2<FMT, true>(w0);
-            const f32x2_t b0 = values2<FMT, false>(w1), b1 = values2<FMT, true>(w1);
-            o[0][e >> 1] = pack2(a0.x * sc.y, b0.x * sc.y);
-            o[1][e >> 1] = pack2(a0.y * sc.y, b0.y * sc.y);
-            o[2][e >> 1] = pack2(a1.x * sc.y, b1.x * sc.y);
-            o[3][e >> 1] = pack2(a1.y * sc.y, b1.y * sc.y);
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (row + i < here) store16(vo + (row + i) * a.row_stride, o[i]);
-    }
+    for (int i = 0; i < 4; ++i)
+        if (row + i < here) store16(vo + i * a.row_stride, o[i]);
 }
 
 template <int FMT, int META>
@@ -559,7 +559,7 @@ extern "C" ss_status ss_read_kv8(const void *kv_base, const int64_t *region_off,
     SS_CHECK_ARG(kv_base && region_off && open_blocks && len && row_begin && k && v, "ss_read_kv8: null pointer");
     SS_CHECK_ARG(aligned16(kv_base) && aligned16(open_blocks) && aligned16(k) && aligned16(v),
                  "ss_read_kv8: buffers must be 16-byte aligned");
-    const int64_t teams = ((int64_t)B + rows / blk) * Hkv, groups = groups_of(teams, blk, read_threads(blk));
+    const int64_t teams = ((int64_t)B + rows / std::min(blk, 16)) * Hkv, groups = groups_of(teams, blk, read_threads(blk));
     SS_CHECK_SUPPORTED(groups <= 0x7FFFFFFF / read_threads(blk), "ss_read_kv8: %lld block records pass the launch",
                        (long long)teams);
     const read_args a = {static_cast<const uint8_t *>(kv_base), region_off, tables, max_blocks, slot_limit,
