@@ -12,10 +12,14 @@
 // each step one rounded fp32 operation, so that the result does not depend on
 // the shape of the launch.
 //
-// A team of 64 lanes (32 for blocks of 8) writes one block of one head: 16
-// lanes read 256 B of a token, so K and V of the block are in its registers
-// with two loads per 4 tokens in flight each, the maxima of both are one
-// packed reduction, and the codes leave as 16-byte stores.  Teams of
+// A team of 64 lanes (32 for blocks of 8) writes the K or the V tile of one
+// block of one head, and a workgroup is a wave of K teams beside one of V teams:
+// neither tile needs the other, and a wave's chain of dependent loads and its
+// arithmetic set the time of all but the largest calls (both tiles to a team: 8
+// chunks of 256 tokens, blocks of 32, mean keys 12.4 us, now 8.1; one token for
+// each of 64 sequences 4.8 and 4.4; 128k tokens 153 both ways).  16 lanes read
+// 256 B of a token, so the tile is in the team's registers with a load per 4
+// tokens in flight each, and the codes leave as 16-byte stores.  Teams of
 // neighbouring heads are neighbours, so that together they read whole tokens.
 // A team reads back at most 16 tokens of a block (with all of a block of 32 to
 // a team, 7 sequences of 5000 tokens, 2 heads, took 8.6 us, 6.8 so; one of 64k
@@ -119,12 +123,12 @@ __device__ __forceinline__ void store16(uint8_t *p, u32x4_t x)
     __builtin_nontemporal_store(x, reinterpret_cast<u32x4_t *>(p));
 }
 
-// Threads of a workgroup.  A team needs no other, and single waves leave and
-// are replaced soonest: writing 64k tokens of 8 heads with cuboids 74.4 us with
-// 256 threads, 71.5 with 64; reading 64k tokens 82.0 and 79.3.  Only reads of
-// blocks of 8, whose teams write half as many rows each, are better off in
-// company (8 x 8k tokens 48.3 and 50.7).
-constexpr int kWriteThreads = 64;
+// Threads of a workgroup.  A team needs no other, and small workgroups leave
+// and are replaced soonest: writing 64k tokens of 8 heads with cuboids 74.4 us
+// with 256 threads, 71.5 with 64 (both tiles to a team); reading 64k tokens 82.0
+// and 79.3.  Only reads of blocks of 8, whose teams write half as many rows
+// each, are better off in company (8 x 8k tokens 48.3 and 50.7).
+constexpr int kWriteThreads = 128;
 constexpr int read_threads(int blk) { return blk == 8 ? 256 : 64; }
 
 struct write_args {
@@ -150,7 +154,8 @@ __global__ __launch_bounds__(kWriteThreads) void write_kernel(const write_args a
     constexpr int NR = 4 * SUB;  // rows of a lane
     constexpr int REC = ss::kv8_record(BLK), OPEN = 2 * BLK * D * 2;
     const int lane = threadIdx.x & 63, tl = lane % TEAM, x = lane & 15, L = tl >> 4;
-    const uint32_t team = (blockIdx.x * kWriteThreads + threadIdx.x) / TEAM, item = team / (uint32_t)a.Hkv;
+    const bool is_v = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t team = (blockIdx.x * 64 + lane) / TEAM, item = team / (uint32_t)a.Hkv;
     const int g = (int)(team - item * (uint32_t)a.Hkv);
     const int b = ss::find_item<BLK, TEAM>(a.tok_begin, a.B, item, lane);
     const int64_t u = (int64_t)b * a.Hkv + g;
@@ -164,26 +169,25 @@ __global__ __launch_bounds__(kWriteThreads) void write_kernel(const write_args a
     const int full = (p0 + n) / BLK;  // blocks that fill
     if (m >= max(full, 1)) return;
     uint8_t *open = a.open + u * OPEN;
-    const uint8_t *kh = a.k + g * a.head_stride + x * 16, *vh = a.v + g * a.head_stride + x * 16;
+    const uint8_t *src = (is_v ? a.v : a.k) + g * a.head_stride + x * 16;
 
     if (full > 0) {
-        u32x4_t K[NR], V[NR];
+        u32x4_t R[NR];
         const int i0 = tb + m * BLK - p0;  // the token of the block's row 0
         // where the block goes, beside its rows and not after them
         int last = a.slots[i0 + BLK - 1], pos = META == kNoMeta ? 0 : a.positions[i0 + BLK - 1];
         const int held = m == 0 ? p0 : 0;  // rows of the open record
-        const uint8_t *k0 = kh + (int64_t)(i0 + 4 * L) * a.tok_stride, *v0 = vh + (int64_t)(i0 + 4 * L) * a.tok_stride;
+        const uint8_t *src0 = src + (int64_t)(i0 + 4 * L) * a.tok_stride;
 #pragma unroll
         for (int r = 0; r < NR; ++r) {
             const int row = (r >> 2) * 16 + 4 * L + (r & 3);
             const int64_t at = ((r >> 2) * 16 + (r & 3)) * a.tok_stride;
-            const uint8_t *kp = k0 + at, *vp = v0 + at;
-            if (row < held) kp = vp = open + row * (D * 2) + x * 16;  // V is replaced below
-            K[r] = load16_stream(kp);
-            V[r] = load16_stream(vp);
+            const uint8_t *p = src0 + at;
+            if (row < held) p = open + row * (D * 2) + x * 16;  // V is replaced below
+            R[r] = load16_stream(p);
         }
         asm volatile("" : "+v"(last), "+v"(pos), "+v"(region));
-        if (held > 0) {
+        if (is_v && held > 0) {
             const uint8_t *ov = open + BLK * D * 2;
 #pragma unroll
             for (int s = 0; s < SUB; ++s) {
@@ -197,22 +201,18 @@ __global__ __launch_bounds__(kWriteThreads) void write_kernel(const write_args a
 #pragma unroll
                         for (int h = 0; h < 4; ++h) {
                             const uint32_t lo = w[2 * h][i >> 1], hi = w[2 * h + 1][i >> 1];
-                            V[4 * s + i][h] = i & 1 ? (lo >> 16) | (hi & 0xFFFF0000u) : (lo & 0xFFFFu) | (hi << 16);
+                            R[4 * s + i][h] = i & 1 ? (lo >> 16) | (hi & 0xFFFF0000u) : (lo & 0xFFFFu) | (hi << 16);
                         }
                     }
             }
         }
-        // largest magnitudes of both tiles, K in the low half
-        uint32_t mk = 0, mv = 0;
+        uint32_t m2 = 0;  // largest magnitudes of both halves
 #pragma unroll
         for (int r = 0; r < NR; ++r)
 #pragma unroll
-            for (int h = 0; h < 4; ++h) {
-                mk = max2(mk, K[r][h] & 0x7FFF7FFFu);
-                mv = max2(mv, V[r][h] & 0x7FFF7FFFu);
-            }
-        const uint32_t mm = team_max2<TEAM>(max2((mk & 0xFFFFu) | (mv << 16), (mk >> 16) | (mv & 0xFFFF0000u)));
-        const tile_scale<FMT> sk(mm & 0xFFFFu), sv(mm >> 16);
+            for (int h = 0; h < 4; ++h) m2 = max2(m2, R[r][h] & 0x7FFF7FFFu);
+        m2 = team_max2<TEAM>(m2);
+        const tile_scale<FMT> sc(max(m2 & 0xFFFFu, m2 >> 16));
 
         const int page = last / BLK;
         if (last >= 0 && page < a.slot_limit && last % BLK == BLK - 1) {
@@ -220,63 +220,65 @@ __global__ __launch_bounds__(kWriteThreads) void write_kernel(const write_args a
 #pragma unroll
             for (int s = 0; s < SUB; ++s) {
                 uint8_t *kt = rec + s * T * D, *vt = rec + BLK * D + s * T * D;
-                // rows 4L + 2j and 4L + 2j + 1: the even lane of a pair takes
-                // both lanes' channels of the first, the odd one of the second
-                const bool odd = x & 1;
-                u32x4_t o[2];
+                if (!is_v) {
+                    // rows 4L + 2j and 4L + 2j + 1: the even lane of a pair takes
+                    // both lanes' channels of the first, the odd one of the second
+                    const bool odd = x & 1;
+                    u32x4_t o[2];
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    uint32_t c[2][2];
+                    for (int j = 0; j < 2; ++j) {
+                        uint32_t c[2][2];
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        const u32x4_t w = K[4 * s + 2 * j + i];
-                        c[i][0] = codes4<FMT>(channel(w, 0), channel(w, 1), channel(w, 2), channel(w, 3), sk.inv) & sk.keep;
-                        c[i][1] = codes4<FMT>(channel(w, 4), channel(w, 5), channel(w, 6), channel(w, 7), sk.inv) & sk.keep;
+                        for (int i = 0; i < 2; ++i) {
+                            const u32x4_t w = R[4 * s + 2 * j + i];
+                            c[i][0] = codes4<FMT>(channel(w, 0), channel(w, 1), channel(w, 2), channel(w, 3), sc.inv) & sc.keep;
+                            c[i][1] = codes4<FMT>(channel(w, 4), channel(w, 5), channel(w, 6), channel(w, 7), sc.inv) & sc.keep;
+                        }
+                        const uint32_t r0 = ss::pair_swap(odd ? c[0][0] : c[1][0]), r1 = ss::pair_swap(odd ? c[0][1] : c[1][1]);
+                        o[j] = odd ? u32x4_t{r0, r1, c[1][0], c[1][1]} : u32x4_t{c[0][0], c[0][1], r0, r1};
                     }
-                    const uint32_t r0 = ss::pair_swap(odd ? c[0][0] : c[1][0]), r1 = ss::pair_swap(odd ? c[0][1] : c[1][1]);
-                    o[j] = odd ? u32x4_t{r0, r1, c[1][0], c[1][1]} : u32x4_t{c[0][0], c[0][1], r0, r1};
-                }
-                // the team's halves exchange, so that a store has 8 (a team of
-                // 32: 4) consecutive tokens of every 16 channels, whole lines
+                    // the team's halves exchange, so that a store has 8 (a team of
+                    // 32: 4) consecutive tokens of every 16 channels, whole lines
 #pragma unroll
-                for (int h = 0; h < 4; ++h) {
-                    const auto y = TEAM == 64 ? __builtin_amdgcn_permlane32_swap(o[0][h], o[1][h], false, false)
-                                              : __builtin_amdgcn_permlane16_swap(o[0][h], o[1][h], false, false);
-                    o[0][h] = y[0];
-                    o[1][h] = y[1];
-                }
-                constexpr int HALF = TEAM / 32;  // lane rows of half a team
-                uint8_t *kl = kt + (x >> 1) * (T * 16) + (4 * (L % HALF) + 2 * (L / HALF) + (odd ? 1 : 0)) * 16;
-                asm("" : "+v"(o[0]), "+v"(o[1]));  // else the two stores lose their policy on the way to the assembly
-                store16(kl, o[0]);
-                store16(kl + HALF * 64, o[1]);
+                    for (int h = 0; h < 4; ++h) {
+                        const auto y = TEAM == 64 ? __builtin_amdgcn_permlane32_swap(o[0][h], o[1][h], false, false)
+                                                  : __builtin_amdgcn_permlane16_swap(o[0][h], o[1][h], false, false);
+                        o[0][h] = y[0];
+                        o[1][h] = y[1];
+                    }
+                    constexpr int HALF = TEAM / 32;  // lane rows of half a team
+                    uint8_t *kl = kt + (x >> 1) * (T * 16) + (4 * (L % HALF) + 2 * (L / HALF) + (odd ? 1 : 0)) * 16;
+                    asm("" : "+v"(o[0]), "+v"(o[1]));  // else the two stores lose their policy in compilation
+                    store16(kl, o[0]);
+                    store16(kl + HALF * 64, o[1]);
+                } else {
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    u32x4_t o;
+                    for (int h = 0; h < 2; ++h) {
+                        u32x4_t o;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        o[e] = codes4<FMT>(channel(V[4 * s], 4 * h + e), channel(V[4 * s + 1], 4 * h + e),
-                                           channel(V[4 * s + 2], 4 * h + e), channel(V[4 * s + 3], 4 * h + e), sv.inv) & sv.keep;
-                    store16(vt + h * (T * 64) + L * 256 + x * 16, o);
+                        for (int e = 0; e < 4; ++e)
+                            o[e] = codes4<FMT>(channel(R[4 * s], 4 * h + e), channel(R[4 * s + 1], 4 * h + e),
+                                               channel(R[4 * s + 2], 4 * h + e), channel(R[4 * s + 3], 4 * h + e), sc.inv) & sc.keep;
+                        store16(vt + h * (T * 64) + L * 256 + x * 16, o);
+                    }
                 }
             }
-            if (tl < ss::kKv8Trailer / 16) {
-                u32x4_t o = {0, 0, 0, 0};
-                if (tl == 0) o = u32x4_t{__float_as_uint(sk.scale), __float_as_uint(sv.scale), 0, 0};
-                store16(rec + 2 * BLK * D + tl * 16, o);
-            }
+            uint8_t *trailer = rec + 2 * BLK * D;  // the zeros come with the V scale
+            if (tl == 0) reinterpret_cast<float *>(trailer)[is_v] = sc.scale;
+            if (is_v && tl == 0) *reinterpret_cast<u32x2_t *>(trailer + 8) = u32x2_t{0, 0};
+            if (is_v && tl > 0 && tl < ss::kKv8Trailer / 16) store16(trailer + tl * 16, u32x4_t{0, 0, 0, 0});
         }
-        if (META != kNoMeta) {
+        if (META != kNoMeta && !is_v) {
             const int jb = pos / BLK;
             const bool live = pos >= 0 && jb < a.nblk_max;
             if (META == SS_META_CUBOID) {
                 u32x4_t o;
 #pragma unroll
                 for (int h = 0; h < 4; ++h) {
-                    uint32_t lo = ss::key2(K[0][h]), nhi = ~lo;
+                    uint32_t lo = ss::key2(R[0][h]), nhi = ~lo;
 #pragma unroll
                     for (int r = 1; r < NR; ++r) {
-                        const uint32_t key = ss::key2(K[r][h]);
+                        const uint32_t key = ss::key2(R[r][h]);
                         lo = ss::min2(lo, key);
                         nhi = ss::min2(nhi, ~key);
                     }
@@ -302,8 +304,8 @@ __global__ __launch_bounds__(kWriteThreads) void write_kernel(const write_args a
                 for (int r = 0; r < NR; ++r)
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        const auto y = TEAM == 64 ? __builtin_amdgcn_permlane32_swap(K[r][h], K[r][2 + h], false, false)
-                                                  : __builtin_amdgcn_permlane16_swap(K[r][h], K[r][2 + h], false, false);
+                        const auto y = TEAM == 64 ? __builtin_amdgcn_permlane32_swap(R[r][h], R[r][2 + h], false, false)
+                                                  : __builtin_amdgcn_permlane16_swap(R[r][h], R[r][2 + h], false, false);
                         t[2 * r][h] = y[0];
                         t[2 * r + 1][h] = y[1];
                     }
@@ -339,10 +341,9 @@ __global__ __launch_bounds__(kWriteThreads) void write_kernel(const write_args a
         __threadfence_block();  // its reads are done
         const int from = full ? 0 : p0, i0 = tb + full * BLK - p0;
         uint16_t *ov = reinterpret_cast<uint16_t *>(open + BLK * D * 2);
-        for (int r = 2 * from + L; r < 2 * rest; r += TEAM / 16) {  // K row, V row of each token
-            const int row = r >> 1;
-            const u32x4_t w = load16((r & 1 ? vh : kh) + (int64_t)(i0 + row) * a.tok_stride);
-            if (r & 1) {
+        for (int row = from + L; row < rest; row += TEAM / 16) {
+            const u32x4_t w = load16(src + (int64_t)(i0 + row) * a.tok_stride);
+            if (is_v) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
                     ov[(8 * x + e) * BLK + row] = (uint16_t)(e & 1 ? w[e >> 1] >> 16 : w[e >> 1] & 0xFFFFu);
@@ -529,7 +530,7 @@ extern "C" ss_status ss_write_kv8(const void *k, const void *v, int64_t tok_stri
     SS_CHECK_ARG(k && v && tok_begin && slots && kv_base && region_off && open_blocks, "ss_write_kv8: null pointer");
     SS_CHECK_ARG(aligned16(k) && aligned16(v) && aligned16(kv_base) && aligned16(open_blocks) && aligned16(meta),
                  "ss_write_kv8: buffers must be 16-byte aligned");
-    const int64_t teams = ((int64_t)B + token_cap / blk) * Hkv, groups = groups_of(teams, blk, kWriteThreads);
+    const int64_t teams = ((int64_t)B + token_cap / blk) * Hkv, groups = groups_of(teams, blk, 64);
     SS_CHECK_SUPPORTED(groups <= 0x7FFFFFFF / kWriteThreads, "ss_write_kv8: %lld block records pass the launch",
                        (long long)teams);
     const write_args a = {static_cast<const uint8_t *>(k), static_cast<const uint8_t *>(v), tok_stride, head_stride,
