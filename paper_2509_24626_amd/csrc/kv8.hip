@@ -21,9 +21,10 @@
 // 256 B of a token, so the tile is in the team's registers with a load per 4
 // tokens in flight each, and the codes leave as 16-byte stores.  Teams of
 // neighbouring heads are neighbours, so that together they read whole tokens.
-// A team reads back at most 16 tokens of a block (with all of a block of 32 to
-// a team, 7 sequences of 5000 tokens, 2 heads, took 8.6 us, 6.8 so; one of 64k
-// tokens, 8 heads, 79 and 77).
+// Reading back is split the same way, and a team takes at most 16 tokens (64k
+// tokens, 8 heads, blocks of 16 77.5 us with both tiles to a team, now 71; 7
+// sequences of up to 5000, 2 heads, blocks of 32 8.6 with a block to a team, now
+// 7.0).  Larger workgroups gain nothing, and single waves take 73 us.
 // HBM bounds it: 512 B in and 256 B (and 8 per token for the trailer at 16
 // tokens a block) out per token and head, and the block's metadata.
 #include <algorithm>
@@ -123,13 +124,7 @@ __device__ __forceinline__ void store16(uint8_t *p, u32x4_t x)
     __builtin_nontemporal_store(x, reinterpret_cast<u32x4_t *>(p));
 }
 
-// Threads of a workgroup.  A team needs no other, and small workgroups leave
-// and are replaced soonest: writing 64k tokens of 8 heads with cuboids 74.4 us
-// with 256 threads, 71.5 with 64 (both tiles to a team); reading 64k tokens 82.0
-// and 79.3.  Only reads of blocks of 8, whose teams write half as many rows
-// each, are better off in company (8 x 8k tokens 48.3 and 50.7).
-constexpr int kWriteThreads = 128;
-constexpr int read_threads(int blk) { return blk == 8 ? 256 : 64; }
+constexpr int kThreads = 128;  // of a workgroup
 
 struct write_args {
     const uint8_t *k, *v;
@@ -147,7 +142,7 @@ struct write_args {
 constexpr int kNoMeta = -1;
 
 template <int BLK, int FMT, int META>
-__global__ __launch_bounds__(kWriteThreads) void write_kernel(const write_args a)
+__global__ __launch_bounds__(kThreads) void write_kernel(const write_args a)
 {
     constexpr int TEAM = BLK == 8 ? 32 : 64;
     constexpr int SUB = BLK == 32 ? 2 : 1, T = BLK / SUB;
@@ -393,13 +388,14 @@ __device__ __forceinline__ u32x2_t row4(uint32_t w, float s)
 }
 
 template <int BLK, int FMT>
-__global__ __launch_bounds__(read_threads(BLK)) void read_kernel(const read_args a)
+__global__ __launch_bounds__(kThreads) void read_kernel(const read_args a)
 {
     constexpr int TEAM = BLK == 8 ? 32 : 64;
     constexpr int SUB = BLK == 32 ? 2 : 1, T = BLK / SUB;  // a team reads a subtile
     constexpr int REC = ss::kv8_record(BLK), OPEN = 2 * BLK * D * 2;
     const int lane = threadIdx.x & 63, tl = lane % TEAM, x = lane & 15, L = tl >> 4;
-    const uint32_t team = (blockIdx.x * read_threads(BLK) + threadIdx.x) / TEAM, item = team / (uint32_t)a.Hkv;
+    const bool is_v = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t team = (blockIdx.x * 64 + lane) / TEAM, item = team / (uint32_t)a.Hkv;
     const int g = (int)(team - item * (uint32_t)a.Hkv);
     const int b = ss::find_item<T, TEAM>(a.row_begin, a.B, item, lane);
     const int64_t u = (int64_t)b * a.Hkv + g;
@@ -411,17 +407,20 @@ __global__ __launch_bounds__(read_threads(BLK)) void read_kernel(const read_args
     const int i0 = (int)i64 * T, here = min(n - i0, T);  // rows from i0 on
     const int j = i0 / BLK, s = SUB == 1 ? 0 : i0 % BLK / T;
     const int64_t out0 = (int64_t)(rb + i0) * a.row_stride + g * a.head_stride + x * 16;
-    uint8_t *ko = a.k + out0, *vo = a.v + out0;
+    uint8_t *out = (is_v ? a.v : a.k) + out0;
     if (j >= len / BLK) {  // the open record's rows
         const uint8_t *open = a.open + u * OPEN;
         const uint16_t *ov = reinterpret_cast<const uint16_t *>(open + BLK * D * 2);
         for (int r = L; r < here; r += TEAM / 16) {
             const int p = s * T + r;
-            store16(ko + r * a.row_stride, load16(open + p * (D * 2) + x * 16));
             u32x4_t w;
+            if (is_v) {
 #pragma unroll
-            for (int h = 0; h < 4; ++h) w[h] = ov[(8 * x + 2 * h) * BLK + p] | (uint32_t)ov[(8 * x + 2 * h + 1) * BLK + p] << 16;
-            store16(vo + r * a.row_stride, w);
+                for (int h = 0; h < 4; ++h) w[h] = ov[(8 * x + 2 * h) * BLK + p] | (uint32_t)ov[(8 * x + 2 * h + 1) * BLK + p] << 16;
+            } else {
+                w = load16(open + p * (D * 2) + x * 16);
+            }
+            store16(out + r * a.row_stride, w);
         }
         return;
     }
@@ -430,48 +429,47 @@ __global__ __launch_bounds__(read_threads(BLK)) void read_kernel(const read_args
     asm volatile("" : "+v"(region));  // loaded beside the table's entry, not after it
     const bool ok = page >= 0 && page < a.slot_limit;
     const uint8_t *rec = a.kv + region + (int64_t)(ok ? page : 0) * REC;
-    u32x4_t K[2] = {}, V[2] = {};
-    f32x2_t sc = {0.f, 0.f};
+    u32x4_t c[2] = {};
+    float scale = 0.f;
     if (ok) {
-        sc = *reinterpret_cast<const f32x2_t *>(rec + 2 * BLK * D);
+        scale = reinterpret_cast<const float *>(rec + 2 * BLK * D)[is_v];
         const uint8_t *kt = rec + s * T * D + (x >> 1) * (T * 16) + (4 * L + (x & 1)) * 16;
         const uint8_t *vt = rec + BLK * D + s * T * D + L * 256 + x * 16;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) K[i] = load16(kt + i * 32);
-#pragma unroll
-        for (int i = 0; i < 2; ++i) V[i] = load16(vt + i * (T * 64));
+        for (int i = 0; i < 2; ++i) c[i] = load16(is_v ? vt + i * (T * 64) : kt + i * 32);
     }
-    const int row = 4 * L;
-    ko += row * a.row_stride;
-    vo += row * a.row_stride;
-    // a lane holds 16 channels of one of two rows; the pair exchanges so that each has 8 of both
+    u32x4_t o[4];  // rows 4L .. 4L + 3
+    if (is_v) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const u32x4_t w = K[i];
-        const bool odd = x & 1;
-        const uint32_t r0 = ss::pair_swap(odd ? w[0] : w[2]), r1 = ss::pair_swap(odd ? w[1] : w[3]);
+        for (int e = 0; e < 8; e += 2) {  // channels 8x + e, 8x + e + 1
+            const uint32_t w0 = c[e >> 2][e & 3], w1 = c[e >> 2][(e & 3) + 1];
+            const f32x2_t a0 = values2<FMT, false>(w0), a1 = values2<FMT, true>(w0);
+            const f32x2_t b0 = values2<FMT, false>(w1), b1 = values2<FMT, true>(w1);
+            o[0][e >> 1] = pack2(a0.x * scale, b0.x * scale);
+            o[1][e >> 1] = pack2(a0.y * scale, b0.y * scale);
+            o[2][e >> 1] = pack2(a1.x * scale, b1.x * scale);
+            o[3][e >> 1] = pack2(a1.y * scale, b1.y * scale);
+        }
+    } else {
+        // a lane holds 16 channels of one of two rows; the pair exchanges so that each has 8 of both
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {  // rows row + 2i + h
-            const bool mine = odd == (h == 1);
-            const u32x2_t lo = row4<FMT>(mine ? (odd ? w[2] : w[0]) : r0, sc.x);
-            const u32x2_t hi = row4<FMT>(mine ? (odd ? w[3] : w[1]) : r1, sc.x);
-            if (row + 2 * i + h < here) store16(ko + (2 * i + h) * a.row_stride, u32x4_t{lo.x, lo.y, hi.x, hi.y});
+        for (int i = 0; i < 2; ++i) {
+            const u32x4_t w = c[i];
+            const bool odd = x & 1;
+            const uint32_t r0 = ss::pair_swap(odd ? w[0] : w[2]), r1 = ss::pair_swap(odd ? w[1] : w[3]);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const bool mine = odd == (h == 1);
+                const u32x2_t lo = row4<FMT>(mine ? (odd ? w[2] : w[0]) : r0, scale);
+                const u32x2_t hi = row4<FMT>(mine ? (odd ? w[3] : w[1]) : r1, scale);
+                o[2 * i + h] = u32x4_t{lo.x, lo.y, hi.x, hi.y};
+            }
         }
     }
-    u32x4_t o[4];
-#pragma unroll
-    for (int e = 0; e < 8; e += 2) {  // channels 8x + e, 8x + e + 1
-        const uint32_t w0 = V[e >> 2][e & 3], w1 = V[e >> 2][(e & 3) + 1];
-        const f32x2_t a0 = values2<FMT, false>(w0), a1 = values2<FMT, true>(w0);
-        const f32x2_t b0 = values2<FMT, false>(w1), b1 = values2<FMT, true>(w1);
-        o[0][e >> 1] = pack2(a0.x * sc.y, b0.x * sc.y);
-        o[1][e >> 1] = pack2(a0.y * sc.y, b0.y * sc.y);
-        o[2][e >> 1] = pack2(a1.x * sc.y, b1.x * sc.y);
-        o[3][e >> 1] = pack2(a1.y * sc.y, b1.y * sc.y);
-    }
+    out += 4 * L * a.row_stride;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-        if (row + i < here) store16(vo + i * a.row_stride, o[i]);
+        if (4 * L + i < here) store16(out + i * a.row_stride, o[i]);
 }
 
 template <int FMT, int META>
@@ -497,12 +495,8 @@ ss_status check_kv8(const char *who, int B, int Hkv, int blk, int d, int fmt, in
 
 bool aligned16(const void *p) { return ((uintptr_t)p & 15) == 0; }
 
-// workgroups of `threads` threads; a team is 64 of them, 32 for blocks of 8
-int64_t groups_of(int64_t teams, int blk, int threads)
-{
-    const int per = threads / (blk == 8 ? 32 : 64);
-    return (teams + per - 1) / per;
-}
+// workgroups; a team is 64 lanes of each of its waves, 32 for blocks of 8
+int64_t groups_of(int64_t teams, int blk) { return blk == 8 ? (teams + 1) / 2 : teams; }
 
 }  // namespace
 
@@ -530,8 +524,8 @@ extern "C" ss_status ss_write_kv8(const void *k, const void *v, int64_t tok_stri
     SS_CHECK_ARG(k && v && tok_begin && slots && kv_base && region_off && open_blocks, "ss_write_kv8: null pointer");
     SS_CHECK_ARG(aligned16(k) && aligned16(v) && aligned16(kv_base) && aligned16(open_blocks) && aligned16(meta),
                  "ss_write_kv8: buffers must be 16-byte aligned");
-    const int64_t teams = ((int64_t)B + token_cap / blk) * Hkv, groups = groups_of(teams, blk, 64);
-    SS_CHECK_SUPPORTED(groups <= 0x7FFFFFFF / kWriteThreads, "ss_write_kv8: %lld block records pass the launch",
+    const int64_t teams = ((int64_t)B + token_cap / blk) * Hkv, groups = groups_of(teams, blk);
+    SS_CHECK_SUPPORTED(groups <= 0x7FFFFFFF / kThreads, "ss_write_kv8: %lld block records pass the launch",
                        (long long)teams);
     const write_args a = {static_cast<const uint8_t *>(k), static_cast<const uint8_t *>(v), tok_stride, head_stride,
                           tok_begin, slots, positions, B, Hkv, token_cap, static_cast<uint8_t *>(kv_base), region_off,
@@ -542,7 +536,7 @@ extern "C" ss_status ss_write_kv8(const void *k, const void *v, int64_t tok_stri
         kernel = e4m3 ? write_of<SS_KV8_E4M3, SS_META_CUBOID>(blk) : write_of<SS_KV8_INT8, SS_META_CUBOID>(blk);
     else if (meta)
         kernel = e4m3 ? write_of<SS_KV8_E4M3, SS_META_MEAN>(blk) : write_of<SS_KV8_INT8, SS_META_MEAN>(blk);
-    ss::launch(kernel, dim3((unsigned)groups), dim3(kWriteThreads), ss::as_stream(stream), a);
+    ss::launch(kernel, dim3((unsigned)groups), dim3(kThreads), ss::as_stream(stream), a);
     return ss::check_launch("ss_write_kv8");
 }
 
@@ -560,13 +554,13 @@ extern "C" ss_status ss_read_kv8(const void *kv_base, const int64_t *region_off,
     SS_CHECK_ARG(kv_base && region_off && open_blocks && len && row_begin && k && v, "ss_read_kv8: null pointer");
     SS_CHECK_ARG(aligned16(kv_base) && aligned16(open_blocks) && aligned16(k) && aligned16(v),
                  "ss_read_kv8: buffers must be 16-byte aligned");
-    const int64_t teams = ((int64_t)B + rows / std::min(blk, 16)) * Hkv, groups = groups_of(teams, blk, read_threads(blk));
-    SS_CHECK_SUPPORTED(groups <= 0x7FFFFFFF / read_threads(blk), "ss_read_kv8: %lld block records pass the launch",
+    const int64_t teams = ((int64_t)B + rows / std::min(blk, 16)) * Hkv, groups = groups_of(teams, blk);
+    SS_CHECK_SUPPORTED(groups <= 0x7FFFFFFF / kThreads, "ss_read_kv8: %lld block records pass the launch",
                        (long long)teams);
     const read_args a = {static_cast<const uint8_t *>(kv_base), region_off, tables, max_blocks, slot_limit,
                          static_cast<const uint8_t *>(open_blocks), len, row_begin, B, Hkv, rows, static_cast<uint8_t *>(k),
                          static_cast<uint8_t *>(v), row_stride, head_stride, teams};
     auto *kernel = fmt == SS_KV8_E4M3 ? read_of<SS_KV8_E4M3>(blk) : read_of<SS_KV8_INT8>(blk);
-    ss::launch(kernel, dim3((unsigned)groups), dim3(read_threads(blk)), ss::as_stream(stream), a);
+    ss::launch(kernel, dim3((unsigned)groups), dim3(kThreads), ss::as_stream(stream), a);
     return ss::check_launch("ss_read_kv8");
 }
