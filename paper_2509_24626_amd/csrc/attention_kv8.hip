@@ -24,7 +24,9 @@
 //   16 channels a load; its accumulators are tokens 4L .. 4L+3 of both
 //   subtiles, and those tokens' codes are its V operand, channels 8*col + t.
 //
-// HBM bounds it (256 bytes and a share of the trailer a token and head).  Each
+// HBM bounds it (256 bytes and a share of the trailer a token and head): 64
+// sequences of 128 selected blocks of 16, 8 heads, take 44.4 us (6.2 TB/s), 16
+// of 8k to 64k tokens 192 us (6.5), one of 128k 47 us with its join (5.8).  Each
 // wave keeps two steps in flight; a CU has about 40 KB of loads in flight
 // whatever the waves ask for (3 or 4 steps in flight gain nothing), so what
 // counts is that all CUs have work.  Pages are resolved 64 entries at a time, an

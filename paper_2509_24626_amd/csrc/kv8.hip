@@ -26,7 +26,9 @@
 // sequences of up to 5000, 2 heads, blocks of 32 8.6 with a block to a team, now
 // 7.0).  Larger workgroups gain nothing, and single waves take 73 us.
 // HBM bounds it: 512 B in and 256 B (and 8 per token for the trailer at 16
-// tokens a block) out per token and head, and the block's metadata.
+// tokens a block) out per token and head, and the block's metadata: 128k tokens
+// of 8 heads with cuboids 154 us, 5.5 TB/s, read and write together (a large
+// copy moves 4.9); reading 64k tokens back 71 us, 5.7 TB/s.
 #include <algorithm>
 
 #include "bf16_keys.hpp"
