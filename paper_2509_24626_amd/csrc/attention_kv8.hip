@@ -49,7 +49,7 @@ constexpr int TOK = 32;  // tokens of a step
 constexpr int WAVES = 4;
 constexpr int CUS = 256;
 constexpr int kShares = 512;  // workgroups of SHARE, two a CU
-constexpr int kShareUnits = 40, kShareSteps = 512;  // from which they share (plan())
+constexpr int kShareUnits = 16, kShareSteps = 224, kShareAll = 24576;  // from which they share (plan())
 constexpr float kNone = -3e38f;  // the maximum of no tokens
 constexpr float kLag = 4.f;       // p may grow to 2^kLag before its maximum is taken anew,
 constexpr float kMostV = 2048.f;  // V scales times gain to this: their product stays within 2^15, in f16's range
@@ -712,13 +712,14 @@ struct split_plan {
 };
 
 // SHARE where a call attends to all blocks of sequences whose lengths only the
-// GPU knows, and there are enough units to cover all CUs with long pieces (us,
-// SPLIT and SHARE, lengths from an eighth of the longest on): 44 units of up
-// to 512 steps 31.0, 28.9; 128 of 512 77.5, 70.7; 44 of 2048 103, 76; 64 of
-// 2048 129, 120; a real batch of 128 of 2048 220, 180.  Few units are split
-// evenly anyway (32 of 512 21.7, 23.2; 12 of 2048 35.3, 37.7), and where a
-// share has several units their beginnings add up (512 of 128 68.6, 73.2; 128
-// of 128 23.9, 26.2).
+// GPU knows, and there is enough work to make up for its longer start (about 3
+// us: the line, a second unit begun within a share, the join).  us, SPLIT and
+// SHARE, lengths from an eighth of the longest on: 16 units of up to 2048 steps
+// 37.7, 32.3; 96 of 256 30.5, 25.1; 128 of 256 33.4, 33.1; 512 of 300 124, 116.
+// Less work: 64 of 320 25.3, 28.8; 16 of 1024 23.9, 27.5; short units, of which
+// a share has several: 162 of 126 24.9, 28.7; 614 of 170 95, 109.  Over 275
+// shapes of 8 to 624 units, 91 to 4096 steps, these three lines lose 0.9%
+// against the better of both on average, 14% at most; SPLIT alone 4% and 40%.
 //
 // SPLIT takes the splits that cost least by a model of the time (us; fitted to
 // 1875 shapes of 1 to 1024 units, 1 to 4096 steps, G 1 to 16, each block size
@@ -734,7 +735,8 @@ split_plan plan(int64_t units, int k, int blk, int G, bool selected, size_t room
     const int steps = (int)(((int64_t)k * blk + TOK - 1) / TOK);
     const int64_t all = units * steps;
     const size_t part = G * kPartHead * sizeof(float);
-    if (!selected && units >= kShareUnits && steps >= kShareSteps && all <= 0x7FFFFFFF && room >= 2 * kShares * part)
+    if (!selected && units >= kShareUnits && steps >= kShareSteps && all >= kShareAll && all <= 0x7FFFFFFF &&
+        room >= 2 * kShares * part)
         return {SHARE, kShares, 0};
     constexpr float kStepHbm = 0.00096f, kRound1 = 0.73f, kRound2 = 1.6f, kRound3 = 0.84f, kGroup = 0.2f, kBoth = 0.088f;
     constexpr float kJoin = 2.61f, kJoinSplit = 0.012f, kJoinGroup = 0.00045f, kJoinHead = 0.00012f;

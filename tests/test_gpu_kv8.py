@@ -727,7 +727,7 @@ def test_attention_of_infinite_open_values(ss):
 def test_two_streams_at_once(ss):
     """Calls that overlap, each with its own workspace: the results of calls alone."""
     rng = np.random.default_rng(55)
-    sets = [Stored(rng, 16, 0, [3000 * 16 + 3, 70 * 16], 2, 4).to_device(), Stored(rng, 8, 1, [2100 * 8] * 14, 3, 4).to_device()]
+    sets = [Stored(rng, 16, 0, [3000 * 16 + 3, 70 * 16], 2, 4).to_device(), Stored(rng, 8, 1, [2500 * 8] * 14, 3, 4).to_device()]
     alone = [attend(ss, s, None, s.max_blocks, with_open=True) for s in sets]
     torch.cuda.synchronize()
     streams, got = [torch.cuda.Stream(), torch.cuda.Stream()], [[], []]
@@ -908,7 +908,7 @@ def test_attention_of_long_tables_shared_out(ss, blk, fmt, B, hkv, G, longest):
     length = (longest * blk * rng.random(B) ** 3).astype(int)
     length[rng.integers(B)] = longest * blk
     length[0] = 0
-    k = max(longest, 512 * 32 // blk)
+    k = max(longest, 700 * 32 // blk)
     s = Stored(rng, blk, fmt, length, hkv, G).to_device()
     first = attend(ss, s, None, k, with_open=True)
     worst = s.check(first, lambda b, g: range(s.nblk[b]), True)
