@@ -487,10 +487,10 @@ ss_status ss_read_kv8(const void *kv_base, const int64_t *region_off, const int3
  * open_blocks and len (device int32 [B]; both or neither): the len[b] % blk
  * tokens of the open record are attended too, in bf16.  With no token the
  * output is 0.  fp32 accumulation; codes and open tokens enter the products
- * exactly, queries but for what lies 2^-38 below a head's largest, and
- * probabilities with 23 bits, down to 2^-35 of the largest (a token of smaller
- * weight than that counts as 0; the V scales of a unit weigh in, so one tile
- * is weighed so beside the unit's largest).
+ * exactly.  A query value is off by at most 2^-39 of its head's largest (by
+ * nothing down to 2^-31 of it); a product of a probability and a V scale by at
+ * most 2^-23 of itself or 2^-35 of the largest such product of its head,
+ * whichever is more; a probability below 2^-126 of the largest may count as 0.
  * An infinity among the V values of an open token gives an infinity or NaN in
  * its channel, in no other.
  *   q: device bf16 [B][Hq][d], out: device fp32 [B][Hq][d]

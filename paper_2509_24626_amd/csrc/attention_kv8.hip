@@ -10,13 +10,15 @@
 // by putting the byte into the low bits of 1024 + 128 + code) and the tiles'
 // scales go where they cost one multiplication a token: K's into the logit, V's
 // into the probability.  Queries become f16 by a power of two for each head,
-// which keeps bf16's 8 bits; p * scale enters as two f16 parts, by a power of two
-// for the wave's largest V scale, which keep 23 bits of it.  (With bf16 operands
-// and three parts a step took 211 vector instructions, e4m3, and 340, int8; now
-// 126 and 222: 11 requests of 512 selected blocks of 8 17.4 us, now 16.4; 64 x
-// 128 blocks 47.2, now 45.6.)
-// The maximum that p is relative to stays as it is until a logit passes it by
-// more than kLag, so that most steps exchange nothing between lanes.
+// which leaves a channel off by at most 2^-39 of the largest; p * scale enters as
+// two f16 parts, by a power of two for each head that follows the head's largest
+// p * scale so far, which leaves a product off by at most 2^-23 of itself or 2^-35
+// of that largest.  (A power of two for the largest scale alone, whatever its
+// weight, let a tile of no weight take the others' bits: all of them beyond a
+// scale of 2^35 times theirs.)  With bf16 operands and three parts a step took 211
+// vector instructions, e4m3, and 340, int8; now 125 and 221.
+// What p and its products are relative to stays as it is until one of them grows
+// to kMost, so that most steps exchange nothing between lanes.
 // The record's order of codes (kv8.hpp) makes a load instruction 1 KiB of
 // consecutive bytes and leaves each lane with its own operand bytes, so
 // nothing passes through LDS either:
@@ -51,8 +53,8 @@ constexpr int CUS = 256;
 constexpr int kShares = 512;  // workgroups of SHARE, two a CU
 constexpr int kShareUnits = 16, kShareSteps = 224, kShareAll = 24576;  // from which they share (plan())
 constexpr float kNone = -3e38f;  // the maximum of no tokens
-constexpr float kLag = 4.f;       // p may grow to 2^kLag before its maximum is taken anew,
-constexpr float kMostV = 2048.f;  // V scales times gain to this: their product stays within 2^15, in f16's range
+constexpr float kMost = 32768.f;  // the largest p * scale (within f16's range) and sum of a step's p
+constexpr int kTop = 10;          // to 2^kTop .. 2^(kTop + 1) the largest p * scale is taken anew
 constexpr int kMaxSplits = 256;
 constexpr int kMaxPartials = 4096;  // units * splits, where there is more than one split
 
@@ -122,6 +124,9 @@ __device__ __forceinline__ uint32_t pack_f16(float x, float y)
 
 // 1/x of a power of two between 2^-126 and 2^126
 __device__ __forceinline__ float inverse(float x) { return __uint_as_float((254u << 23) - __float_as_uint(x)); }
+
+// 127 and the exponent of a float of no sign
+__device__ __forceinline__ int exponent(float x) { return (int)(__float_as_uint(x) >> 23); }
 
 // maximum over the four 16-lane rows, in every lane
 __device__ __forceinline__ float rows_max(float x)
@@ -252,7 +257,7 @@ __global__ __launch_bounds__(WAVES * 64, MODE == SPLIT ? 3 : 2) void attn_kv8_ke
     constexpr int EPS = TOK / BLK;        // entries of a step
     constexpr int SET = 64 / EPS;         // steps of a set of 64 entries
     // the waves' partial results, and that of the open record
-    __shared__ float sm_m[WAVES + 1][16], sm_l[WAVES + 1][16], sm_g[WAVES + 1];
+    __shared__ float sm_m[WAVES + 1][16], sm_l[WAVES + 1][16], sm_g[WAVES + 1][16];
     __shared__ __align__(16) float sm_o[WAVES + 1][16][D + 4];
 
     const int lane = threadIdx.x & 63;
@@ -319,22 +324,26 @@ __global__ __launch_bounds__(WAVES * 64, MODE == SPLIT ? 3 : 2) void attn_kv8_ke
             return st < s_end && e < n_entries && block < blocks && page < limit ? page : -1;
         };
 
-        // Softmax state of head `col`: mref, the maximum that p is relative to;
+        // Softmax state of head `col`: mref, a whole number that p is relative to;
         // lrun, the lane's sum of p; gain, a power of two that the V scales are
-        // multiplied by, so that p * scale is in f16's range.
+        // multiplied by, so that p * scale is in f16's range and the largest so
+        // far at least 2^kTop.
         float mref = kNone, lrun = 0.f, gain = 0x1p126f;
         f32x4_t o[8];
 #pragma unroll
         for (int t = 0; t < 8; ++t) o[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-        // a partial result to LDS; the lane holds channels 32L + 8i + t of head `col`
+        // a partial result to LDS; the lane holds channels 32L + 8i + t of head `col`.
+        // mref may lie far below the largest logit, so the sum is taken to [1, 2):
+        // the outputs are then of V's size.
         auto put = [&](int place) {
             float l = lrun + __shfl_xor(lrun, 16);
             l += __shfl_xor(l, 32);
+            const int e = place < WAVES ? max(exponent(l) - 127, 0) : 0;
             if (L == 0) {
-                sm_m[place][col] = mref;
-                sm_l[place][col] = l;
+                sm_m[place][col] = mref + (float)e;
+                sm_l[place][col] = __builtin_ldexpf(l, -e);
+                sm_g[place][col] = __builtin_ldexpf(1.f, 127 - exponent(gain) - e);
             }
-            if (lane == 0) sm_g[place] = inverse(gain);
             if (col < a.G) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
@@ -400,58 +409,65 @@ __global__ __launch_bounds__(WAVES * 64, MODE == SPLIT ? 3 : 2) void attn_kv8_ke
                     acc[s] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f.h, qf[m].h, acc[s], 0, 0, 0);
                 }
             const float sk[2] = {x.ok[0] ? x.sc[0].x * q_scale : 0.f, x.ok[1] ? x.sc[1].x * q_scale : 0.f};
-            float p[8], sv[2];  // logits relative to mref, then probabilities; V scales times gain
-            auto relate = [&] {
+            float p[8], v[8], sum, top;  // probabilities, times V scales and gain; their sum and the largest of both
+            auto weigh = [&] {
 #pragma unroll
                 for (int s = 0; s < 2; ++s) {
-                    const float bias = x.ok[s] ? -mref : -INFINITY;
+                    const float bias = x.ok[s] ? -mref : -INFINITY, sv = x.sc[s].y * gain;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) p[4 * s + i] = __builtin_fmaf(acc[s][i], sk[s], bias);
-                    sv[s] = x.sc[s].y * gain;
+                    for (int i = 4 * s; i < 4 * s + 4; ++i) {
+                        p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[s][i & 3], sk[s], bias));
+                        v[i] = p[i] * sv;
+                    }
                 }
-                return fmaxf(fmaxf(fmaxf(p[0], p[1]), fmaxf(p[2], p[3])), fmaxf(fmaxf(p[4], p[5]), fmaxf(p[6], p[7])));
+                sum = ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+                top = sum;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) top = fmaxf(top, v[i]);
             };
-            const float top = relate();
-            if (__builtin_expect(__any(top > kLag || fmaxf(sv[0], sv[1]) > kMostV), 0)) {
-                float z = -INFINITY, v = fmaxf(x.sc[0].y, x.sc[1].y);
+            weigh();
+            if (__builtin_expect(__any(top > kMost), 0)) {
+                float z = -INFINITY, y = 0.f;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) z = fmaxf(z, x.ok[i >> 2] ? acc[i >> 2][i & 3] * sk[i >> 2] : -INFINITY);
-                const float mnew = fmaxf(mref, rows_max(z));
-                if (BLK == 8) v = rows_max(v);
-                // the largest scale to [1024, 2048)
-                float gnew = gain;
-                if (v * gain > kMostV) gnew = __uint_as_float((uint32_t)min(254 + 10 - (int)(__float_as_uint(v) >> 23), 253) << 23);
-                const float alpha = __builtin_amdgcn_exp2f(mref - mnew), f = alpha * (gnew * inverse(gain));
+                // whole numbers, so that what is there is rescaled exactly, and not at all
+                // where its largest product stays the largest
+                const float mnew = fmaxf(mref, __builtin_ceilf(rows_max(z)));
+                const int rise = (int)fminf(mnew - mref, 1024.f);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float bias = x.ok[i >> 2] ? -mnew : -INFINITY;
+                    y = fmaxf(y, __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i >> 2][i & 3], sk[i >> 2], bias)) * x.sc[i >> 2].y);
+                }
+                const int gnew = min(min(exponent(gain) + rise, 253), 254 + kTop - exponent(rows_max(y)));
+                const float f = __builtin_ldexpf(1.f, gnew - exponent(gain) - rise);
 #pragma unroll
                 for (int t = 0; t < 8; ++t) o[t] *= f;
-                lrun *= alpha;
+                lrun = __builtin_ldexpf(lrun, -rise);
                 mref = mnew;
-                gain = gnew;
-                relate();
+                gain = __uint_as_float((uint32_t)gnew << 23);
+                weigh();
             }
+            lrun += sum;
             frag_t hi, lo;
 #pragma unroll
             for (int i = 0; i < 8; i += 2) {
-                const float p0 = __builtin_amdgcn_exp2f(p[i]), p1 = __builtin_amdgcn_exp2f(p[i + 1]);
-                lrun += p0;
-                lrun += p1;
-                const float x0 = p0 * sv[i >> 2], x1 = p1 * sv[i >> 2];
-                hi.w[i >> 1] = pack_f16(x0, x1);
-                lo.w[i >> 1] = pack_f16(minus_lo(hi.w[i >> 1], x0), minus_hi(hi.w[i >> 1], x1));
+                hi.w[i >> 1] = pack_f16(v[i], v[i + 1]);
+                lo.w[i >> 1] = pack_f16(minus_lo(hi.w[i >> 1], v[i]), minus_hi(hi.w[i >> 1], v[i + 1]));
             }
             // four accumulators in turn, so that none waits for its last product
 #pragma unroll
             for (int t = 0; t < 8; t += 4) {
-                frag_t v[4];
+                frag_t w[4];
 #pragma unroll
                 for (int h = 0; h < 4; ++h) {
-                    widen4<FMT>(x.v[t >> 2][h], v[h].w[0], v[h].w[1]);
-                    widen4<FMT>(x.v[2 + (t >> 2)][h], v[h].w[2], v[h].w[3]);
+                    widen4<FMT>(x.v[t >> 2][h], w[h].w[0], w[h].w[1]);
+                    widen4<FMT>(x.v[2 + (t >> 2)][h], w[h].w[2], w[h].w[3]);
                 }
 #pragma unroll
-                for (int h = 0; h < 4; ++h) o[t + h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v[h].h, hi.h, o[t + h], 0, 0, 0);
+                for (int h = 0; h < 4; ++h) o[t + h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(w[h].h, hi.h, o[t + h], 0, 0, 0);
 #pragma unroll
-                for (int h = 0; h < 4; ++h) o[t + h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v[h].h, lo.h, o[t + h], 0, 0, 0);
+                for (int h = 0; h < 4; ++h) o[t + h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(w[h].h, lo.h, o[t + h], 0, 0, 0);
                 __builtin_amdgcn_sched_barrier(0);
             }
         };
@@ -597,7 +613,7 @@ __global__ __launch_bounds__(WAVES * 64, MODE == SPLIT ? 3 : 2) void attn_kv8_ke
             for (int w = 0; w < partials; ++w) {
                 const float sc = __builtin_amdgcn_exp2f(sm_m[w][h] - M);
                 lsum += sc * sm_l[w][h];
-                osum += sc * sm_g[w] * *reinterpret_cast<const f32x4_t *>(&sm_o[w][h][ch]);
+                osum += sc * sm_g[w][h] * *reinterpret_cast<const f32x4_t *>(&sm_o[w][h][ch]);
             }
             if (first == 0 && last == nsteps) {
                 if (lsum != 0.f) osum /= lsum;
