@@ -427,18 +427,19 @@ __global__ __launch_bounds__(WAVES * 64, MODE == SPLIT ? 3 : 2) void attn_kv8_ke
             };
             weigh();
             if (__builtin_expect(__any(top > kMost), 0)) {
-                float z = -INFINITY, y = 0.f;
+                float z[2], y = 0.f;  // the subtiles' largest logits; the largest product
 #pragma unroll
-                for (int i = 0; i < 8; ++i) z = fmaxf(z, x.ok[i >> 2] ? acc[i >> 2][i & 3] * sk[i >> 2] : -INFINITY);
+                for (int s = 0; s < 2; ++s) {
+                    z[s] = -INFINITY;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) z[s] = fmaxf(z[s], x.ok[s] ? acc[s][i] * sk[s] : -INFINITY);
+                }
                 // whole numbers, so that what is there is rescaled exactly, and not at all
                 // where its largest product stays the largest
-                const float mnew = fmaxf(mref, __builtin_ceilf(rows_max(z)));
+                const float mnew = fmaxf(mref, __builtin_ceilf(rows_max(fmaxf(z[0], z[1]))));
                 const int rise = (int)fminf(mnew - mref, 1024.f);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float bias = x.ok[i >> 2] ? -mnew : -INFINITY;
-                    y = fmaxf(y, __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i >> 2][i & 3], sk[i >> 2], bias)) * x.sc[i >> 2].y);
-                }
+                for (int s = 0; s < 2; ++s) y = fmaxf(y, __builtin_amdgcn_exp2f(z[s] - mnew) * x.sc[s].y);
                 const int gnew = min(min(exponent(gain) + rise, 253), 254 + kTop - exponent(rows_max(y)));
                 const float f = __builtin_ldexpf(1.f, gnew - exponent(gain) - rise);
 #pragma unroll
