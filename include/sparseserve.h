@@ -490,7 +490,9 @@ ss_status ss_read_kv8(const void *kv_base, const int64_t *region_off, const int3
  * exactly.  A query value is off by at most 2^-39 of its head's largest (by
  * nothing down to 2^-31 of it); a product of a probability and a V scale by at
  * most 2^-23 of itself or 2^-35 of the largest such product of its head,
- * whichever is more; a probability below 2^-126 of the largest may count as 0.
+ * whichever is more; a probability below 2^-125 of the largest may count as 0.
+ * A head whose query holds an infinity or a NaN is NaN where there is a token;
+ * an open token whose logit is -infinity (of an infinite key) counts as none.
  * An infinity among the V values of an open token gives an infinity or NaN in
  * its channel, in no other.
  *   q: device bf16 [B][Hq][d], out: device fp32 [B][Hq][d]

@@ -572,7 +572,7 @@ __global__ __launch_bounds__(WAVES * 64, MODE == SPLIT ? 3 : 2) void attn_kv8_ke
         }
 
         // the queries as f16, times a power of two that takes the head's largest
-        // to [2^14, 2^15): bf16's 8 bits fit, down to 2^-39 of the largest
+        // to [2^14, 2^15): bf16's 8 bits fit down to 2^-31 of it, one down to 2^-38
         {
             uint32_t mag = 0;
 #pragma unroll
@@ -580,7 +580,7 @@ __global__ __launch_bounds__(WAVES * 64, MODE == SPLIT ? 3 : 2) void attn_kv8_ke
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
                     mag = max(mag, max(qf[m].w[i] << 16 & 0x7FFF0000u, qf[m].w[i] & 0x7FFF0000u));
-            const int e = (int)(__float_as_uint(rows_max(__uint_as_float(min(mag, 0x7F800000u)))) >> 23);
+            const int e = exponent(rows_max(__uint_as_float(min(mag, 0x7F800000u))));
             const int to = min(254 + 14 - e, 253);
             const float up = __uint_as_float((uint32_t)to << 23);
             // with an infinity or a NaN among them every logit is NaN (and no skipped entry's)
@@ -603,6 +603,9 @@ __global__ __launch_bounds__(WAVES * 64, MODE == SPLIT ? 3 : 2) void attn_kv8_ke
             compute_step(bufB);
         }
         put(wave);
+        // the open tokens' too: the infinities that they may have got have no softmax,
+        // whatever their signs
+        if (opens && L == 0 && q_scale != q_scale) sm_l[WAVES][col] = q_scale;
         __syncthreads();
         const int partials = tail ? WAVES + 1 : WAVES;
         for (int idx = threadIdx.x; idx < a.G * (D / 4); idx += WAVES * 64) {
