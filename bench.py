@@ -665,7 +665,7 @@ def exit_report():
 # only for the workload and arguments it was taken with, and only while the
 # sources of its kernel hash as they did then; otherwise traffic is null.
 KERNEL_SOURCES = {
-    "gather": ["gather.hip", "decode.cpp"],
+    "gather": ["gather.hip", "kv8.hpp", "decode.cpp"],
     "score": ["score.hip", "score_tile.hpp"],
     "topk": ["topk.hip", "score_tile.hpp"],
     "attention": ["attention.hip"],
@@ -674,7 +674,7 @@ KERNEL_SOURCES = {
 # 2,4,10,20,18,8,2, host resolve
 _KEY = ["hier-b64-ctx128k-blk16-k128-cache25", 0, 20, [2, 4, 10, 20, 18, 8, 2], "host"]
 TRAFFIC = {
-    "gather": {"key": _KEY, "digest": "7c66147e955c4f70", "bytes": 245799069, "fetch": 123711645,
+    "gather": {"key": _KEY, "digest": "7c2549d906f4115f", "bytes": 245799069, "fetch": 123711645,
               "write": 122087424},
     "score": {"key": _KEY, "digest": "2e132a6e12c33d33", "bytes": 2168457152, "fetch": 2151679904,
               "write": 16777248},
