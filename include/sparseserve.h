@@ -395,8 +395,8 @@ ss_status ss_append_kv(const void *new_kv, int32_t *len_dev, int32_t *nblk_dev, 
  *       past token_cap.
  *       A row that is not served takes nothing and keeps its length.
  * A page number outside the pool (in tables or free_pages) gives slots of -1.
- * B up to 65536; n_pages * blk below 2^31.  One launch up to 4096 token rows,
- * else two.
+ * B up to 65536 (with B = 0 nothing is written); n_pages * blk below 2^31.  One
+ * launch up to 4096 token rows, else two.
  * ss_block_release returns the pages of finished rows (done: device int32
  * [B], non-zero) to the stack, row after row in block order, and sets their
  * length to 0; other rows keep theirs.  tables is not written.  len_out may

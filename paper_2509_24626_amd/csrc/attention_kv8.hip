@@ -27,8 +27,9 @@
 //   subtiles, and those tokens' codes are its V operand, channels 8*col + t.
 //
 // HBM bounds it (256 bytes and a share of the trailer a token and head): 64
-// sequences of 128 selected blocks of 16, 8 heads, take 44.4 us (6.2 TB/s), 16
-// of 8k to 64k tokens 192 us (6.5), one of 128k 47 us with its join (5.8).  Each
+// sequences of 128 selected blocks of 16, 8 heads, take 45 us (6.2 TB/s), 16 of 8k
+// to 64k tokens 194 us (6.5), one of 128k 47 to 56 us with its join, by where its
+// records lie in memory (5.8 to 4.9; the kernel alone 45 to 51).  Each
 // wave keeps two steps in flight; a CU has about 40 KB of loads in flight
 // whatever the waves ask for (3 or 4 steps in flight gain nothing), so what
 // counts is that all CUs have work.  Pages are resolved 64 entries at a time, an
@@ -750,6 +751,9 @@ struct split_plan {
 //     kRound1 alone on the CU, kRound2 beside another, kRound3 for each of more;
 //     kGroup a workgroup besides;
 //   - the join, a second launch.
+// The ranges follow from k, not from the lengths: 8k tokens of one request, 8
+// heads, blocks of 16, take 10.1 us with k = 513, 12.6 with 2048 and 24.3 with
+// 8192, where two of 32 splits have work (of eight requests 25.7 and 26.2).
 split_plan plan(int64_t units, int k, int blk, int G, bool selected, size_t room)
 {
     const int steps = (int)(((int64_t)k * blk + TOK - 1) / TOK);
