@@ -109,3 +109,21 @@ def test_values_near_the_largest(ss, blk):  # noqa: F811
     for page in range(s.n):
         scale_of(s, 0, page, 1)[:] = np.float32(2.0 ** 111)
     check(ss, s, 4096 // blk)
+
+
+@pytest.mark.parametrize("fmt, G", [(0, 7), (1, 16)])
+def test_large_tiles_where_steps_are_shared_out(ss, fmt, G):  # noqa: F811
+    """Tables long enough that 512 workgroups share the steps of all sequences,
+    each of which has a tile of 2^40 times the others' V scale and no weight."""
+    rng = np.random.default_rng(G)
+    blk = 32
+    s = Stored(rng, blk, fmt, [blk * int(n) for n in rng.integers(1, 60, 14)], 2, G)
+    s.q = np.abs(s.q)
+    for b in range(1, s.B):
+        page = s.tables[b, rng.integers(s.nblk[b])]
+        if s.nblk[b] > 1:
+            codes = s.rec[b % 2, page, :blk * D]
+            codes[:] = -np.abs(codes.view(np.int8)).view(np.uint8) if fmt else codes | 0x80  # negative keys
+            scale_of(s, b % 2, page, 0)[:] *= np.float32(16)
+            scale_of(s, b % 2, page, 1)[:] *= np.float32(2.0 ** 40)
+    check(ss, s, 900)
